@@ -9,6 +9,8 @@
  *   psa_attention_fwd    Sec. 3.4, Alg. 1, Eq. 8   online-softmax attention over mixed-level KV blocks
  *   psa_attention_bwd    Sec. 1 (claim), derived from Eq. 8 and Eq. 2-3   gradients of the above
  *   psa_dense_ref        Sec. 3.1, Eq. 1     plain softmax attention (reference / comparison)
+ * and, around them in a layer of the models that they are for:
+ *   psa_rotary           rotary positions with several axes (time, height, width) of Q and K, and their inverse
  *
  * Conventions for every call
  *   - Every pointer is a DEVICE pointer owned by the caller unless it says "host".  The library
@@ -109,6 +111,49 @@ int psa_build_pyramid(const psa_params* p, const void* K, const void* V, void* K
 int psa_hilbert_order(int32_t T, int32_t Hg, int32_t W, int32_t* perm);
 int psa_permute_tokens(const psa_params* p, int32_t heads, const void* X, const int32_t* perm,
                        int32_t inverse, void* Y, void* stream);
+
+/*
+ * Rotary positions with several axes: what turns Q and K before psa_build_pyramid and the calls after it, and what takes the gradients
+ * of the turned Q and K back.  Channel pair i (i < d / 2) of token t's row turns by  pos[axis[i], t] * freq[i]  radians:
+ *   y0 = x0 cos - x1 sin,  y1 = x0 sin + x1 cos;   pair i is channels (2i, 2i + 1) or (i, i + d / 2).
+ * The angle is worked out in 64 bits, the rotation in fp32 (sine and cosine to 2^-23), rounded once to dtype.
+ *   forward (inverse = 0)   out[b, h, k, :] = R(t) in[b, h, t, :],   t = perm ? perm[k] : k
+ *   inverse (inverse != 0)  out[b, h, t, :] = R(t)^T in[b, h, k, :]
+ * so that one pass turns the tokens as the projection left them and puts them in the order of psa_hilbert_order.  The side that has the
+ * tokens in their own order (a forward call's inputs, an inverse one's outputs) may have any strides, the other is contiguous [B, heads, N, d].
+ *
+ * psa_rotary_spec, filled by the caller (zeros first, then psa_rotary_spectrum, or by hand):
+ *   axes        1 .. PSA_ROTARY_MAX_AXES
+ *   pairing     PSA_ROTARY_ADJACENT | PSA_ROTARY_HALVES
+ *   axis        per pair: the axis that turns it, or PSA_ROTARY_STILL: the pair's bits are kept
+ *   freq        per pair: radians a position, at most 2^20 either way
+ *   q_stride, k_stride   elements from one batch entry, head, token to the next on the tokens' side; channels are adjacent.  All three
+ *               0: contiguous [B, heads, N, d].  A projection's [B, N, heads, d] is {N heads d, d, heads d}.  Not negative.  Inputs may
+ *               repeat rows (stride 0); outputs may not: ordered by size, each stride must reach past what the smaller ones cover.
+ * psa_rotary_spectrum (host call): axis and freq of `axes` axes of pairs[0..axes-1] channel pairs each (at most d / 2 in all, the rest
+ *   is PSA_ROTARY_STILL), one axis after the other.  shared = 0: pair j of an axis turns base^(-j / pairs[axis]) (every axis has the
+ *   whole range); shared != 0: pair i of the row turns base^(-i / (d / 2)), whatever its axis.  Sets axes too.
+ *   Errors: PSA_EINVAL (null pointer, d not 64 or 128, axes, pairs or base out of range).
+ * psa_rotary: p supplies B, Hq, Hkv, N, d, dtype.
+ *   pos         DEVICE, int32 [axes, N] of every batch entry, pos_stride elements apart (0: one for all); any sign
+ *   perm        nullable, DEVICE, int32 [N], a permutation of 0..N-1; a row whose entry is out of range is skipped
+ *   Qin, Qout   Q's two sides; both may be NULL: K alone.  Kin, Kout likewise.
+ *   Qout == Qin (Kout == Kin) is allowed where both sides are contiguous and perm is NULL; other overlaps are not.
+ *   Errors: PSA_EINVAL (null pointer, one side of a tensor without the other, pairing, axis, freq or strides out of range, in place
+ *           otherwise), PSA_EUNSUPPORTED (2^31 rows or more), PSA_ELAUNCH.
+ */
+enum { PSA_ROTARY_ADJACENT = 0, PSA_ROTARY_HALVES = 1 };
+#define PSA_ROTARY_MAX_AXES 4
+#define PSA_ROTARY_STILL 255
+typedef struct psa_rotary_spec {
+  int32_t axes, pairing;
+  uint8_t axis[64];
+  double freq[64];
+  int64_t q_stride[3], k_stride[3];
+} psa_rotary_spec;
+int psa_rotary_spectrum(int32_t d, int32_t axes, const int32_t* pairs, double base, int32_t shared, psa_rotary_spec* r);
+int psa_rotary(const psa_params* p, const psa_rotary_spec* r, const int32_t* pos, int64_t pos_stride, const int32_t* perm, int32_t inverse,
+               const void* Qin, const void* Kin, void* Qout, void* Kout, void* stream);
 
 /*
  * Cosine-similarity pooling constraint, App. B.1 / Alg. 3: the maximum admissible level of every key

@@ -11,6 +11,8 @@ PSA_REP_STRIDED, PSA_REP_POOLED = 0, 1
 PSA_EST_MAX, PSA_EST_MEAN = 0, 1
 PSA_ALLOC_THRESHOLD, PSA_ALLOC_QUANTILE, PSA_ALLOC_BUDGET, PSA_ALLOC_THRESHOLD_EXCL = 0, 1, 2, 3
 PSA_CAP_PER_HEAD, PSA_CAP_ALL_HEADS = 0, 1
+PSA_ROTARY_ADJACENT, PSA_ROTARY_HALVES = 0, 1
+PSA_ROTARY_MAX_AXES, PSA_ROTARY_STILL = 4, 255
 PSA_MAX_LEVELS = 8
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -44,6 +46,14 @@ class PsaParams(ctypes.Structure):
         return -(-self.N // self.bk)
 
 
+class PsaRotary(ctypes.Structure):
+    """Mirror of `psa_rotary_spec` in include/psa.h (see make_rotary)."""
+    _fields_ = [
+        ("axes", ctypes.c_int32), ("pairing", ctypes.c_int32), ("axis", ctypes.c_uint8 * 64), ("freq", ctypes.c_double * 64),
+        ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3),
+    ]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -65,6 +75,9 @@ def load_library() -> ctypes.CDLL:
     fp = ctypes.POINTER(ctypes.c_float)
     lib.psa_hilbert_order.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(ctypes.c_int32)]
     lib.psa_permute_tokens.argtypes = [pp, ctypes.c_int32, vp, vp, ctypes.c_int32, vp, vp]
+    rp = ctypes.POINTER(PsaRotary)
+    lib.psa_rotary_spectrum.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(ctypes.c_int32), ctypes.c_double, ctypes.c_int32, rp]
+    lib.psa_rotary.argtypes = [pp, rp, vp, ctypes.c_int64, vp, ctypes.c_int32, vp, vp, vp, vp, vp]
     lib.psa_level_cap.argtypes = [pp, vp, fp, ctypes.c_int, vp, vp, vp]
     lib.psa_build_pyramid_cap.argtypes = [pp, vp, vp, vp, vp, fp, ctypes.c_int, vp, vp, vp]
     lib.psa_allocate_levels.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
@@ -79,7 +92,7 @@ def load_library() -> ctypes.CDLL:
     lib.psa_status_str.restype = ctypes.c_char_p
     for name in ("psa_query_sizes", "psa_build_pyramid", "psa_allocate_levels", "psa_attention_fwd", "psa_attention_fwd_static",
                  "psa_level_cap", "psa_build_pyramid_cap", "psa_query_bwd_sizes", "psa_attention_bwd", "psa_hilbert_order", "psa_permute_tokens",
-                 "psa_dense_ref", "psa_probe_copy", "psa_probe_mfma"):
+                 "psa_dense_ref", "psa_probe_copy", "psa_probe_mfma", "psa_rotary_spectrum", "psa_rotary"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -152,6 +165,84 @@ def psa_permute_tokens(p: PsaParams, X, perm, Y, inverse: bool = False, stream=N
     _check(load_library().psa_permute_tokens(ctypes.byref(p), ctypes.c_int32(heads), _ptr(X), _ptr(perm),
                                              ctypes.c_int32(1 if inverse else 0), _ptr(Y), _stream(stream)),
            "psa_permute_tokens")
+
+
+def _strides_of(x) -> Tuple[int, int, int]:
+    """Strides (batch, head, token) that a spec gets: of a [B, H, L, d] tensor or view, as a tuple, or None (contiguous)."""
+    if x is None:
+        return (0, 0, 0)
+    if isinstance(x, (tuple, list)):
+        b, h, n = x
+        return (int(b), int(h), int(n))
+    if x.dim() != 4 or x.stride(3) != 1:
+        raise ValueError("libpsa takes [B, H, L, d] tensors whose channels are adjacent")
+    return (0, 0, 0) if x.is_contiguous() else tuple(x.stride()[:3])
+
+
+def _dtype_of(p: PsaParams):
+    import torch
+    return torch.bfloat16 if p.dtype == PSA_BF16 else torch.float32
+
+
+def _rows(x, shape, dtype, strides, device):
+    """Device pointer of a [B, H, L, d] tensor that the kernels address by `strides` ((0, 0, 0): contiguous)."""
+    if x is None:
+        return None
+    if x.shape != shape or x.dtype != dtype:
+        raise ValueError(f"expected a {dtype} tensor of shape {tuple(shape)}, got {x.dtype} {tuple(x.shape)}")
+    if x.device != device:
+        raise ValueError("libpsa takes tensors of the current device")
+    if strides == (0, 0, 0):
+        if not x.is_contiguous():
+            raise ValueError("the tensor is not contiguous: give its strides to the spec")
+    elif x.numel():
+        for n, want, got in zip(shape, strides + (1,), x.stride()):
+            if n > 1 and want != got:
+                raise ValueError(f"the tensor's strides {x.stride()} are not the spec's {strides}")
+    return x.data_ptr()
+
+
+def _table(x, shapes, dtype, device, what):
+    """Device pointer of a contiguous table (None stays NULL)."""
+    if x is None:
+        return None
+    if x.dtype != dtype or tuple(x.shape) not in shapes or x.device != device or not x.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous {dtype} tensor of shape {' or '.join(map(str, shapes))} on the current device")
+    return x.data_ptr()
+
+
+def _here():
+    import torch
+    return torch.device("cuda", torch.cuda.current_device())
+
+
+def make_rotary(d: int, pairs: Sequence[int], base: float = 10000.0, shared: bool = False, pairing: int = PSA_ROTARY_ADJACENT,
+                q=None, k=None) -> PsaRotary:
+    """Spec of psa_rotary: `pairs` channel pairs per axis (psa_rotary_spectrum); q, k: the tensors on the tokens' side, or their
+    strides (batch, head, token), where those are not contiguous."""
+    r = PsaRotary()
+    n = (ctypes.c_int32 * max(len(pairs), 1))(*pairs)
+    _check(load_library().psa_rotary_spectrum(d, len(pairs), n, base, 1 if shared else 0, ctypes.byref(r)), "psa_rotary_spectrum")
+    r.pairing = pairing
+    r.q_stride, r.k_stride = _strides_of(q), _strides_of(k)
+    return r
+
+
+def psa_rotary(p: PsaParams, r: PsaRotary, pos, Qin, Kin, Qout, Kout, perm=None, inverse: bool = False, stream=None) -> None:
+    """Q and K ([B, heads, N, d], either may be None on both sides) turned by pos (int32 [axes, N], [1, axes, N] or [B, axes, N])."""
+    import torch
+    dev, dt = _here(), _dtype_of(p)
+    q, k, tight = tuple(r.q_stride), tuple(r.k_stride), (0, 0, 0)
+    sq, sk = (p.B, p.Hq, p.N, p.d), (p.B, p.Hkv, p.N, p.d)
+    shapes = ((r.axes, p.N), (1, r.axes, p.N), (p.B, r.axes, p.N))
+    at = _table(pos, shapes, torch.int32, dev, "pos")
+    if at is None:
+        raise ValueError("pos is needed")
+    _check(load_library().psa_rotary(
+        ctypes.byref(p), ctypes.byref(r), at, r.axes * p.N if pos.dim() == 3 and pos.shape[0] > 1 else 0,
+        _table(perm, ((p.N,),), torch.int32, dev, "perm"), 1 if inverse else 0,
+        _rows(Qin, sq, dt, tight if inverse else q, dev), _rows(Kin, sk, dt, tight if inverse else k, dev),
+        _rows(Qout, sq, dt, q if inverse else tight, dev), _rows(Kout, sk, dt, k if inverse else tight, dev), _stream(stream)), "psa_rotary")
 
 
 def _thresholds(p: PsaParams, tau_s: Sequence[float]):

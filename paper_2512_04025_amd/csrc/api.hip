@@ -141,6 +141,32 @@ bool lists_in_kernel(const Plan& pl, bool descriptors) {
   return pl.N <= 5120 && pl.N * (workgroups > 512 ? workgroups : 512) <= 5120 * 512;
 }
 
+bool make_strides(const int64_t* s, int B, int H, int64_t L, int d, bool written, Strides* out) {
+  if (s[0] == 0 && s[1] == 0 && s[2] == 0) {
+    *out = {H * L * d, L * d, d};
+    return true;
+  }
+  struct Axis { int64_t step, n; } ax[3] = {{s[0], B}, {s[1], H}, {s[2], L}};
+  for (int i = 0; i < 3; ++i)
+    if (ax[i].step < 0 || ax[i].step > ((int64_t)1 << 56) / (ax[i].n > 0 ? ax[i].n : 1)) return false;
+  *out = {s[0], s[1], s[2]};
+  if (!written) return true;
+  for (int i = 0; i < 2; ++i)                      // by size
+    for (int j = 0; j < 2 - i; ++j)
+      if (ax[j].step > ax[j + 1].step) {
+        const Axis x = ax[j];
+        ax[j] = ax[j + 1];
+        ax[j + 1] = x;
+      }
+  int64_t covered = d;
+  for (int i = 0; i < 3; ++i) {
+    if (ax[i].n <= 1) continue;
+    if (ax[i].step < covered) return false;
+    covered += ax[i].step * (ax[i].n - 1);
+  }
+  return true;
+}
+
 static inline char* at(void* base, size_t off) { return static_cast<char*>(base) + off; }
 
 }  // namespace psa
@@ -181,6 +207,45 @@ int psa_permute_tokens(const psa_params* p, int32_t heads, const void* X, const 
   if (rc != PSA_OK) return rc;
   if (heads <= 0 || heads > 65535 || !X || !perm || !Y || X == Y) return PSA_EINVAL;
   return launch_permute(pl, heads, X, perm, inverse != 0, Y, static_cast<hipStream_t>(stream)) == hipSuccess ? PSA_OK : PSA_ELAUNCH;
+}
+
+int psa_rotary_spectrum(int32_t d, int32_t axes, const int32_t* pairs, double base, int32_t shared, psa_rotary_spec* r) {
+  if (!pairs || !r || (d != 64 && d != 128) || axes < 1 || axes > PSA_ROTARY_MAX_AXES) return PSA_EINVAL;
+  if (!(base >= 1.0) || isinf(base)) return PSA_EINVAL;
+  int64_t sum = 0;
+  for (int ax = 0; ax < axes; ++ax) {
+    if (pairs[ax] < 0) return PSA_EINVAL;
+    sum += pairs[ax];
+  }
+  if (sum > d / 2) return PSA_EINVAL;
+  rotary_spectrum_host(d, axes, pairs, base, shared != 0, r);
+  return PSA_OK;
+}
+
+int psa_rotary(const psa_params* p, const psa_rotary_spec* r, const int32_t* pos, int64_t pos_stride, const int32_t* perm, int32_t inverse,
+               const void* Qin, const void* Kin, void* Qout, void* Kout, void* stream) {
+  Plan pl;
+  const int rc = make_plan(p, &pl);
+  if (rc != PSA_OK) return rc;
+  if (!r || !pos || pos_stride < 0 || pos_stride > ((int64_t)1 << 56) / pl.B) return PSA_EINVAL;
+  if ((!Qin != !Qout) || (!Kin != !Kout) || (!Qin && !Kin)) return PSA_EINVAL;
+  if (r->axes < 1 || r->axes > PSA_ROTARY_MAX_AXES || (r->pairing != PSA_ROTARY_ADJACENT && r->pairing != PSA_ROTARY_HALVES)) return PSA_EINVAL;
+  for (int i = 0; i < pl.d / 2; ++i) {
+    if (r->axis[i] == PSA_ROTARY_STILL) continue;
+    if (r->axis[i] >= r->axes || !(fabs(r->freq[i]) <= 1048576.0)) return PSA_EINVAL;
+  }
+  const int Hq = Qin ? pl.Hq : 0, Hkv = Kin ? pl.Hkv : 0;
+  Strides q = {0, 0, 0}, k = {0, 0, 0};
+  if (Qin && !make_strides(r->q_stride, pl.B, pl.Hq, pl.N, pl.d, inverse != 0, &q)) return PSA_EINVAL;
+  if (Kin && !make_strides(r->k_stride, pl.B, pl.Hkv, pl.N, pl.d, inverse != 0, &k)) return PSA_EINVAL;
+  auto tight = [&](const Strides& x, int H) {
+    return (x.n == pl.d || pl.N == 1) && (x.h == (int64_t)pl.N * pl.d || H == 1) && (x.b == (int64_t)H * pl.N * pl.d || pl.B == 1);
+  };
+  if (Qin && Qin == Qout && (perm || !tight(q, pl.Hq))) return PSA_EINVAL;
+  if (Kin && Kin == Kout && (perm || !tight(k, pl.Hkv))) return PSA_EINVAL;
+  if ((int64_t)pl.B * pl.N > 0x7fffffff / ((int64_t)Hq + Hkv)) return PSA_EUNSUPPORTED;
+  return launch_rotary(pl, *r, Hq, Hkv, q, k, pos, pos_stride, perm, inverse != 0, Qin, Kin, Qout, Kout, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? PSA_OK : PSA_ELAUNCH;
 }
 
 static int check_cap_args(const Plan& pl, const float* tau_s, int reduce, const float* sim, const uint8_t* L) {

@@ -28,6 +28,11 @@ struct Plan {
 
 int make_plan(const psa_params* p, Plan* out);
 
+// Elements from one batch entry, head, token to the next of a tensor whose channels are adjacent.
+struct Strides { int64_t b, h, n; };
+// s: as the caller gave them (all 0: contiguous [B, H, L, d]).  written: no two rows may meet.  False: refused.
+bool make_strides(const int64_t* s, int B, int H, int64_t L, int d, bool written, Strides* out);
+
 // LDS a workgroup may use on gfx950, and the one-time opt-in that lets a kernel ask for more than the
 // default 64 KB of dynamic LDS.  The limit is raised to the hardware maximum once per kernel and
 // device (never lowered again), so concurrent calls with different problem sizes cannot shrink each
@@ -60,6 +65,11 @@ hipError_t launch_level_cap(const Plan& pl, const float* sims, const float* tau_
 // Hilbert-curve token order of a T x Hg x W grid (host) and the row gather / scatter that applies it
 int hilbert_order_host(int T, int Hg, int W, int32_t* perm);
 hipError_t launch_permute(const Plan& pl, int heads, const void* X, const int32_t* perm, bool inverse, void* Y, hipStream_t s);
+// Rotary positions of Q (Hq heads) and K (Hkv heads); either count may be 0
+constexpr int ROTARY_PAIRS = 64;
+hipError_t launch_rotary(const Plan& pl, const psa_rotary_spec& r, int Hq, int Hkv, const Strides& q, const Strides& k, const int32_t* pos, int64_t pos_stride,
+                         const int32_t* perm, bool inverse, const void* Qin, const void* Kin, void* Qout, void* Kout, hipStream_t s);
+void rotary_spectrum_host(int d, int axes, const int32_t* pairs, double base, bool shared, psa_rotary_spec* r);
 // Rk (nullable): also the keys'
 hipError_t launch_representatives(const Plan& pl, const void* Q, void* Rq, const void* K, void* Rk, hipStream_t s);
 // part: per (row, key slice) partial softmax statistics of the matrix-core path (Plan::off_part)
