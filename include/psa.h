@@ -10,6 +10,7 @@
  *   psa_attention_bwd    Sec. 1 (claim), derived from Eq. 8 and Eq. 2-3   gradients of the above
  *   psa_dense_ref        Sec. 3.1, Eq. 1     plain softmax attention (reference / comparison)
  * and, around them in a layer of the models that they are for:
+ *   psa_cross_attention_fwd, psa_cross_attention_bwd   attention to the states of an encoder (text, sound, images), and its gradients
  *   psa_rotary           rotary positions with several axes (time, height, width) of Q and K, and their inverse
  *
  * Conventions for every call
@@ -289,6 +290,47 @@ int psa_attention_fwd_static(const psa_params* p, const void* Q, const void* K, 
  */
 int psa_dense_ref(const psa_params* p, const void* Q, const void* K, const void* V, void* O,
                   float* lse, void* stream);
+
+/*
+ * Cross attention: the N query tokens of a head attend to M states of an encoder, another length than their own.
+ *   s_j = scale q . k_j  over the states j that are seen:  j < kv_len[b]  and  key_mask[b, j] != 0
+ *   O = sum softmax(s)_j v_j,   lse = log sum exp(s_j)
+ * A row that sees no state (or none but at a score of -inf) has O = 0 and lse = -inf, and its gradients are 0.  States that are not seen have no influence
+ * whatever their keys and values hold (NaN and infinities too), and their dK, dV are 0.  p supplies B, Hq, Hkv, N, d, dtype and
+ * scale; causal must be 0 (PSA_EINVAL).  The call does not use the pyramid, so that p can be the layer's own.
+ *
+ * psa_cross: M, and per tensor the elements from one batch entry, head, token (state) to the next; channels are adjacent; all three 0:
+ *   contiguous [B, heads, N or M, d].  Not negative.  Inputs may repeat rows (stride 0, states that a batch shares); tensors that are written
+ *   may not: ordered by size, each stride must reach past what the smaller ones cover.  From one state to the next at most 32 MB (backward:
+ *   tokens of Q and dO too).  The d*_stride are read by the backward call only, do_stride is dO's.
+ *   M = 0 is allowed (K, V, dK, dV may then be NULL).
+ * psa_query_cross_sizes (host call): bytes of workspace, either pointer may be NULL.  0 for most forward calls: only where few query
+ *   rows meet many states do workgroups share a row's states and leave partial results there.  256-byte aligned.
+ * psa_cross_attention_fwd
+ *   Q [B, Hq, N, d], K, V [B, Hkv, M, d]; O out
+ *   kv_len      nullable, DEVICE, int32 [B]; below 0 counts as 0, above M as M
+ *   key_mask    nullable, DEVICE, uint8 [B, M]
+ *   lse         nullable out, float [B, Hq, N]
+ *   scratch     may be NULL where none is needed
+ * psa_cross_attention_bwd: the gradients for dO, with P = exp(s - lse), D = dO . O, dS = P (dO V^T - D):
+ *   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO;  query heads that share a key head add up.  Every element of dQ, dK, dV is written.
+ *   O, lse      as the forward call gave them;  dO [B, Hq, N, d]
+ *   Memory of K, V that a batch shares (stride 0): dK, dV are each entry's own.
+ * bfloat16: products on MFMA with fp32 accumulation; P and dS are rounded to bfloat16 for the products that consume them.  float32: fp32
+ * products and sums.  No atomics: bit-reproducible.
+ * Errors: PSA_EINVAL (null pointer, misaligned scratch, M < 0, causal, strides), PSA_EUNSUPPORTED (B * Hkv above 65535, Hq / Hkv * N or M
+ *         above 2^31 - 129, strides above 32 MB), PSA_ELAUNCH.
+ */
+typedef struct psa_cross {
+  int32_t M;
+  int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3], dq_stride[3], dk_stride[3], dv_stride[3], do_stride[3];
+} psa_cross;
+int psa_query_cross_sizes(const psa_params* p, const psa_cross* x, size_t* fwd_scratch, size_t* bwd_scratch);
+int psa_cross_attention_fwd(const psa_params* p, const psa_cross* x, const void* Q, const void* K, const void* V, const int32_t* kv_len,
+                            const uint8_t* key_mask, void* O, float* lse, void* scratch, void* stream);
+int psa_cross_attention_bwd(const psa_params* p, const psa_cross* x, const void* Q, const void* K, const void* V, const int32_t* kv_len,
+                            const uint8_t* key_mask, const void* O, const float* lse, const void* dO, void* dQ, void* dK, void* dV,
+                            void* scratch, void* stream);
 
 /* Static description of a status code (host pointer, never NULL). */
 const char* psa_status_str(int status);

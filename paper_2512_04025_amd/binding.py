@@ -54,6 +54,11 @@ class PsaRotary(ctypes.Structure):
     ]
 
 
+class PsaCross(ctypes.Structure):
+    """Mirror of `psa_cross` in include/psa.h (see make_cross)."""
+    _fields_ = [("M", ctypes.c_int32)] + [(n + "_stride", ctypes.c_int64 * 3) for n in ("q", "k", "v", "o", "dq", "dk", "dv", "do")]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -78,6 +83,10 @@ def load_library() -> ctypes.CDLL:
     rp = ctypes.POINTER(PsaRotary)
     lib.psa_rotary_spectrum.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(ctypes.c_int32), ctypes.c_double, ctypes.c_int32, rp]
     lib.psa_rotary.argtypes = [pp, rp, vp, ctypes.c_int64, vp, ctypes.c_int32, vp, vp, vp, vp, vp]
+    xp = ctypes.POINTER(PsaCross)
+    lib.psa_query_cross_sizes.argtypes = [pp, xp, szp, szp]
+    lib.psa_cross_attention_fwd.argtypes = [pp, xp] + [vp] * 9
+    lib.psa_cross_attention_bwd.argtypes = [pp, xp] + [vp] * 13
     lib.psa_level_cap.argtypes = [pp, vp, fp, ctypes.c_int, vp, vp, vp]
     lib.psa_build_pyramid_cap.argtypes = [pp, vp, vp, vp, vp, fp, ctypes.c_int, vp, vp, vp]
     lib.psa_allocate_levels.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
@@ -92,7 +101,8 @@ def load_library() -> ctypes.CDLL:
     lib.psa_status_str.restype = ctypes.c_char_p
     for name in ("psa_query_sizes", "psa_build_pyramid", "psa_allocate_levels", "psa_attention_fwd", "psa_attention_fwd_static",
                  "psa_level_cap", "psa_build_pyramid_cap", "psa_query_bwd_sizes", "psa_attention_bwd", "psa_hilbert_order", "psa_permute_tokens",
-                 "psa_dense_ref", "psa_probe_copy", "psa_probe_mfma", "psa_rotary_spectrum", "psa_rotary"):
+                 "psa_dense_ref", "psa_probe_copy", "psa_probe_mfma", "psa_rotary_spectrum", "psa_rotary",
+                 "psa_query_cross_sizes", "psa_cross_attention_fwd", "psa_cross_attention_bwd"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -298,6 +308,64 @@ def psa_attention_bwd(p: PsaParams, Q, K, V, Kpyr, Vpyr, M, O, lse, dO, dQ, dK, 
 def psa_dense_ref(p: PsaParams, Q, K, V, O, lse=None, stream=None) -> None:
     _check(load_library().psa_dense_ref(ctypes.byref(p), _ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(lse),
                                         _stream(stream)), "psa_dense_ref")
+
+
+def make_cross(M: int, q=None, k=None, v=None, o=None, dq=None, dk=None, dv=None, do=None) -> PsaCross:
+    """Spec of the cross attention to M states; per tensor the tensor itself ([B, H, L, d], any view with adjacent channels) or its
+    strides (batch, head, token) where it is not contiguous."""
+    x = PsaCross()
+    x.M = M
+    for name, t in (("q", q), ("k", k), ("v", v), ("o", o), ("dq", dq), ("dk", dk), ("dv", dv), ("do", do)):
+        setattr(x, name + "_stride", _strides_of(t))
+    return x
+
+
+def psa_query_cross_sizes(p: PsaParams, x) -> Tuple[int, int]:
+    """(bytes of scratch of the forward call, of the backward call); x: a PsaCross, or just M."""
+    fwd, bwd = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    x = x if isinstance(x, PsaCross) else make_cross(x)
+    _check(load_library().psa_query_cross_sizes(ctypes.byref(p), ctypes.byref(x), ctypes.byref(fwd), ctypes.byref(bwd)), "psa_query_cross_sizes")
+    return fwd.value, bwd.value
+
+
+def _scratch(p: PsaParams, x: PsaCross, scratch, which: int, device):
+    """Device pointer of a workspace that is large enough."""
+    need = psa_query_cross_sizes(p, x)[which]
+    if scratch is None:
+        if need:
+            raise ValueError(f"{need} bytes of scratch are needed")
+        return None
+    if scratch.device != device or not scratch.is_contiguous() or scratch.numel() * scratch.element_size() < need:
+        raise ValueError(f"scratch: a contiguous tensor of {need} bytes on the current device is needed")
+    return scratch.data_ptr()
+
+
+def psa_cross_attention_fwd(p: PsaParams, x: PsaCross, Q, K, V, O, scratch=None, lse=None, kv_len=None, key_mask=None, stream=None) -> None:
+    """Q, O: [B, Hq, N, d]; K, V: [B, Hkv, M, d]; kv_len: int32 [B]; key_mask: uint8 or bool [B, M]; lse: float [B, Hq, N]."""
+    import torch
+    dev, dt = _here(), _dtype_of(p)
+    sq, sk = (p.B, p.Hq, p.N, p.d), (p.B, p.Hkv, x.M, p.d)
+    _check(load_library().psa_cross_attention_fwd(
+        ctypes.byref(p), ctypes.byref(x), _rows(Q, sq, dt, tuple(x.q_stride), dev), _rows(K, sk, dt, tuple(x.k_stride), dev), _rows(V, sk, dt, tuple(x.v_stride), dev),
+        _table(kv_len, ((p.B,),), torch.int32, dev, "kv_len"), _mask(p, x, key_mask, dev), _rows(O, sq, dt, tuple(x.o_stride), dev),
+        _table(lse, ((p.B, p.Hq, p.N),), torch.float32, dev, "lse"), _scratch(p, x, scratch, 0, dev), _stream(stream)), "psa_cross_attention_fwd")
+
+
+def _mask(p: PsaParams, x: PsaCross, key_mask, device):
+    import torch
+    return None if key_mask is None else _table(key_mask, ((p.B, x.M),), torch.bool if key_mask.dtype == torch.bool else torch.uint8, device, "key_mask")
+
+
+def psa_cross_attention_bwd(p: PsaParams, x: PsaCross, Q, K, V, O, lse, dO, dQ, dK, dV, scratch, kv_len=None, key_mask=None, stream=None) -> None:
+    import torch
+    dev, dt = _here(), _dtype_of(p)
+    sq, sk = (p.B, p.Hq, p.N, p.d), (p.B, p.Hkv, x.M, p.d)
+    rows = lambda t, s, name: _rows(t, s, dt, tuple(getattr(x, name)), dev)          # noqa: E731
+    _check(load_library().psa_cross_attention_bwd(
+        ctypes.byref(p), ctypes.byref(x), rows(Q, sq, "q_stride"), rows(K, sk, "k_stride"), rows(V, sk, "v_stride"),
+        _table(kv_len, ((p.B,),), torch.int32, dev, "kv_len"), _mask(p, x, key_mask, dev), rows(O, sq, "o_stride"), _table(lse, ((p.B, p.Hq, p.N),), torch.float32, dev, "lse"),
+        rows(dO, sq, "do_stride"), rows(dQ, sq, "dq_stride"), rows(dK, sk, "dk_stride"), rows(dV, sk, "dv_stride"), _scratch(p, x, scratch, 1, dev), _stream(stream)),
+        "psa_cross_attention_bwd")
 
 
 def psa_probe_copy(src, dst, nbytes: int, stream=None) -> None:

@@ -407,6 +407,85 @@ int psa_attention_bwd(const psa_params* p, const void* Q, const void* K, const v
   return e == hipSuccess ? PSA_OK : PSA_ELAUNCH;
 }
 
+// ---- cross attention
+struct CrossLayout { size_t off_part, off_stats, fwd_bytes, off_D, off_dq, off_dk, off_dv, bwd_bytes; };
+
+static CrossLayout cross_layout(const Plan& pl, int M) {
+  CrossLayout l;
+  const size_t rows = (size_t)pl.B * pl.Hq * pl.N, keys = (size_t)pl.B * pl.Hkv * M, e = sizeof(float);
+  const size_t kp = cross_key_parts(pl, M), rp = cross_row_parts(pl, M);
+  l.off_part = 0;
+  l.off_stats = kp > 1 ? align256(kp * rows * pl.d * e) : 0;
+  l.fwd_bytes = kp > 1 ? l.off_stats + align256(kp * rows * e) : 0;
+  size_t s = 0;
+  l.off_D = s;  s += align256(rows * e);
+  l.off_dq = s; s += kp > 1 ? align256(kp * rows * pl.d * e) : 0;
+  l.off_dk = s; s += rp > 1 ? align256(rp * keys * pl.d * e) : 0;
+  l.off_dv = s; s += rp > 1 ? align256(rp * keys * pl.d * e) : 0;
+  l.bwd_bytes = s;
+  return l;
+}
+
+static int make_cross(const psa_params* p, const psa_cross* x, Plan* pl, CrossCall* c, bool gradients) {
+  const int rc = make_plan(p, pl);
+  if (rc != PSA_OK) return rc;
+  if (!x || x->M < 0 || pl->causal) return PSA_EINVAL;
+  c->M = x->M;
+  const int B = pl->B, Hq = pl->Hq, Hkv = pl->Hkv, N = pl->N, M = x->M, d = pl->d;
+  if (!make_strides(x->q_stride, B, Hq, N, d, false, &c->q) || !make_strides(x->k_stride, B, Hkv, M, d, false, &c->k) ||
+      !make_strides(x->v_stride, B, Hkv, M, d, false, &c->v) || !make_strides(x->o_stride, B, Hq, N, d, !gradients, &c->o)) return PSA_EINVAL;
+  if (gradients && (!make_strides(x->do_stride, B, Hq, N, d, false, &c->go) || !make_strides(x->dq_stride, B, Hq, N, d, true, &c->gq) ||
+                    !make_strides(x->dk_stride, B, Hkv, M, d, true, &c->gk) || !make_strides(x->dv_stride, B, Hkv, M, d, true, &c->gv))) return PSA_EINVAL;
+  // offsets inside a tile of 64 rows are 32 bits wide, and so are the rows of a key head
+  const int64_t most = ((int64_t)1 << 25) / pl->esize;
+  if (c->k.n >= most || c->v.n >= most || (gradients && (c->q.n >= most || c->go.n >= most))) return PSA_EUNSUPPORTED;
+  if ((int64_t)B * Hkv > 65535 || (int64_t)pl->group * N > 0x7fffffff - 128 || M > 0x7fffffff - 128) return PSA_EUNSUPPORTED;
+  return PSA_OK;
+}
+
+int psa_query_cross_sizes(const psa_params* p, const psa_cross* x, size_t* fwd_scratch, size_t* bwd_scratch) {
+  Plan pl;
+  CrossCall c;
+  const int rc = make_cross(p, x, &pl, &c, true);
+  if (rc != PSA_OK) return rc;
+  const CrossLayout l = cross_layout(pl, c.M);
+  if (fwd_scratch) *fwd_scratch = l.fwd_bytes;
+  if (bwd_scratch) *bwd_scratch = l.bwd_bytes;
+  return PSA_OK;
+}
+
+int psa_cross_attention_fwd(const psa_params* p, const psa_cross* x, const void* Q, const void* K, const void* V, const int32_t* kv_len,
+                            const uint8_t* key_mask, void* O, float* lse, void* scratch, void* stream) {
+  Plan pl;
+  CrossCall c;
+  const int rc = make_cross(p, x, &pl, &c, false);
+  if (rc != PSA_OK) return rc;
+  if (!Q || !O || (c.M > 0 && (!K || !V))) return PSA_EINVAL;
+  const CrossLayout l = cross_layout(pl, c.M);
+  if (l.fwd_bytes && (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255))) return PSA_EINVAL;
+  c.kv_len = kv_len;
+  c.key_mask = key_mask;
+  return launch_cross_fwd(pl, c, Q, K, V, O, lse, reinterpret_cast<float*>(at(scratch, l.off_part)), reinterpret_cast<float*>(at(scratch, l.off_stats)),
+                          static_cast<hipStream_t>(stream)) == hipSuccess ? PSA_OK : PSA_ELAUNCH;
+}
+
+int psa_cross_attention_bwd(const psa_params* p, const psa_cross* x, const void* Q, const void* K, const void* V, const int32_t* kv_len,
+                            const uint8_t* key_mask, const void* O, const float* lse, const void* dO, void* dQ, void* dK, void* dV,
+                            void* scratch, void* stream) {
+  Plan pl;
+  CrossCall c;
+  const int rc = make_cross(p, x, &pl, &c, true);
+  if (rc != PSA_OK) return rc;
+  if (!Q || !O || !lse || !dO || !dQ || !scratch || (c.M > 0 && (!K || !V || !dK || !dV))) return PSA_EINVAL;
+  if (reinterpret_cast<uintptr_t>(scratch) & 255) return PSA_EINVAL;
+  const CrossLayout l = cross_layout(pl, c.M);
+  c.kv_len = kv_len;
+  c.key_mask = key_mask;
+  auto f = [&](size_t off) { return reinterpret_cast<float*>(at(scratch, off)); };
+  return launch_cross_bwd(pl, c, Q, K, V, O, lse, dO, dQ, dK, dV, f(l.off_D), f(l.off_dq), f(l.off_dk), f(l.off_dv), static_cast<hipStream_t>(stream)) == hipSuccess
+             ? PSA_OK : PSA_ELAUNCH;
+}
+
 // ---- psa_attention_fwd_static: the same kernels, their workspace in a static device array.
 // In host code the array's name is only a handle for hipGetSymbolAddress: the address the kernels get
 // is looked up once per device (each GPU holds its own copy) and kept in static_ptr.

@@ -1,0 +1,693 @@
+// Cross attention: N query tokens a head against M encoder states, of which batch entry b shows those with j < kv_len[b] and
+// key_mask[b, j] != 0.  With s_j = scale q.k_j:  P = softmax over the states that are seen, O = P V, lse = log sum exp(s).  Backward, with
+// P = exp(s - lse), D = dO.O, dP = dO V^T, dS = P (dP - D):  dQ = scale dS K, dK = scale dS^T Q, dV = P^T dO.
+//
+// All three kernels are made of two products on 32x32 MFMA tiles with fp32 accumulation (see Mma):
+//   rows:  [32 rows of a tile in LDS] x [32 rows in registers]^T   -> one register row in each lane, the tile's rows in its registers
+//   cols:  [32 rows of a tile in LDS]^T x [that result]            -> the result is the second operand as it lies, no lane exchange
+// forward, dQ: the tile is a piece of K or V, the registers hold the query rows; dK, dV: the tile is a piece of Q or dO, the registers hold
+// keys and values.  The query heads of a key head are rows of one matrix (row = head in group * N + token), so that few tokens of many
+// heads fill a tile.  Tiles come straight into LDS, double buffered, one tile ahead; one barrier a tile.
+// No atomics: sums over workgroups are written as partial results and added in a fixed order.
+#include "psa_dev.h"
+#include "psa_internal.h"
+
+namespace psa {
+
+struct CrossArgs {
+  int B, Hq, Hkv, group, N, M;
+  int rows;                                   // group * N: query rows of a key head
+  int parts, tiles_per_part;                  // workgroups that share a row's keys (forward, dQ) or a key's rows (dK, dV)
+  int chunks;                                 // dK, dV: tiles of one head's tokens
+  float scale, scale_log2;
+  Strides q, k, v, o, gq, gk, gv, go;         // g: gradients
+  const int32_t* kv_len;
+  const uint8_t* mask;
+};
+
+constexpr float CROSS_LOG2E = 1.44269504088896340736f, CROSS_LN2 = 0.69314718055994530942f;
+constexpr float CROSS_LAZY = 8.f;             // the running maximum moves when it grows by more than 2^8
+
+typedef __attribute__((ext_vector_type(4))) short cs16x4;
+typedef __attribute__((ext_vector_type(8))) short cs16x8;
+typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
+
+// Tiles are rows of D elements; the 16-byte chunks of a row are permuted (XOR with swz(row), which has period 16), on the way into LDS, so that
+// neither the row reads nor the column reads meet in a bank.
+template <typename T, int D> struct Mma;
+
+template <int D> struct Mma<bf16_t, D> {
+  static constexpr int ROWB = D * 2, CPR = D / 8, KS = D / 16, MD = D / 32, VEC = 8;
+  typedef bf16x8 Frag;
+  static __device__ __forceinline__ int swz(int row) { return row_swizzle32<D>(row); }
+  static __device__ __forceinline__ f32x16 mul(Frag a, Frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  // 32 rows x 32 channels transposed: 16 lanes take 4 rows x 32 bytes, a lane gets one channel of them
+  static __device__ __forceinline__ uint32_t cols_base(int lane) {
+    const int hf = lane >> 5, s16 = lane & 15, row = hf * 4 + (s16 >> 2), chunk = ((lane >> 4) & 1) * 2 + ((s16 & 3) >> 1);
+    return (uint32_t)(row * ROWB + ((chunk ^ swz(row)) << 4) + (s16 & 1) * 8);
+  }
+  static __device__ __forceinline__ cs16x4 read_t(const unsigned char* p) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) cs16x4*)p);
+  }
+  struct Weights { bf16x8 f[2]; };            // rounded once: the products take bfloat16
+  static __device__ __forceinline__ Weights weights(const f32x16& p) {
+    Weights w;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      w.f[i] = __builtin_bit_cast(bf16x8, (u32x4{f32_to_bf16_pair(p[8 * i], p[8 * i + 1]), f32_to_bf16_pair(p[8 * i + 2], p[8 * i + 3]),
+                                                 f32_to_bf16_pair(p[8 * i + 4], p[8 * i + 5]), f32_to_bf16_pair(p[8 * i + 6], p[8 * i + 7])}));
+    return w;
+  }
+  static __device__ __forceinline__ void cols(f32x16 (&acc)[MD], const unsigned char* tile, uint32_t base, const Weights& w) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int md = 0; md < MD; ++md) {
+        const uint32_t x = base ^ (uint32_t)(md << 6);
+        const cs16x4 lo = read_t(tile + i * 16 * ROWB + x), hi = read_t(tile + (i * 16 + 8) * ROWB + (x ^ 32u));
+        acc[md] = mul(__builtin_bit_cast(bf16x8, (cs16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)), w.f[i], acc[md]);
+      }
+  }
+};
+
+template <int D> struct Mma<float, D> {
+  static constexpr int ROWB = D * 4, CPR = D / 4, KS = D / 8, MD = D / 32, VEC = 4;
+  typedef f32x4 Frag;                         // four products of 32x32x2; a lane half has every other chunk
+  static __device__ __forceinline__ int swz(int row) { return row & 15; }
+  static __device__ __forceinline__ f32x16 mul(Frag a, Frag b, f32x16 c) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ uint32_t cols_base(int lane) {
+    const int hf = lane >> 5, l32 = lane & 31;
+    return (uint32_t)(hf * 4 * ROWB + (((l32 >> 2) ^ (hf * 4)) << 4) + (l32 & 3) * 4);
+  }
+  struct Weights { f32x16 f; };
+  static __device__ __forceinline__ Weights weights(const f32x16& p) { return {p}; }
+  static __device__ __forceinline__ void cols(f32x16 (&acc)[MD], const unsigned char* tile, uint32_t base, const Weights& w) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {            // register v: rows (v / 4) * 8 + v % 4 and 4 after it
+      const int row = (v >> 2) * 8 + (v & 3);
+#pragma unroll
+      for (int md = 0; md < MD; ++md) {
+        const float x = *reinterpret_cast<const float*>(tile + row * ROWB + (base ^ (uint32_t)(((row & 15) ^ (md * 8)) << 4)));
+        acc[md] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w.f[v], acc[md], 0, 0, 0);
+      }
+    }
+  }
+};
+
+template <typename T, int D> using RowFrags = typename Mma<T, D>::Frag[Mma<T, D>::KS];
+template <typename T, int D> __device__ __forceinline__ uint32_t rows_base(int lane) {
+  typedef Mma<T, D> X;
+  const int l32 = lane & 31, hf = lane >> 5;
+  return (uint32_t)(l32 * X::ROWB + ((hf ^ X::swz(l32)) << 4));
+}
+template <typename T, int D> __device__ __forceinline__ f32x16 rows(const unsigned char* tile, uint32_t base, const RowFrags<T, D>& f) {
+  typedef Mma<T, D> X;
+  f32x16 acc = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int ks = 0; ks < X::KS; ++ks) acc = X::mul(*reinterpret_cast<const typename X::Frag*>(tile + (base ^ (uint32_t)(ks << 5))), f[ks], acc);
+  return acc;
+}
+// the lane's row (p: its first element) as the operand of rows(); ok: false gives zeros
+template <typename T, int D> __device__ __forceinline__ void row_frags(RowFrags<T, D>& f, const T* p, int hf, bool ok) {
+  typedef Mma<T, D> X;
+#pragma unroll
+  for (int ks = 0; ks < X::KS; ++ks) {
+    u32x4 x = {0u, 0u, 0u, 0u};
+    if (ok) x = *reinterpret_cast<const u32x4_at2*>(p + (2 * ks + hf) * X::VEC);
+    f[ks] = __builtin_bit_cast(typename X::Frag, x);
+  }
+}
+
+// R rows from `base` on, `step` bytes apart, of which `have` exist, straight into LDS at `to`, by NW wavefronts.  Rows that do not exist are out of the
+// descriptor's range; what their places in LDS then hold is not relied on (see blank()).
+template <typename T, int D, int R, int NW> struct Stage {
+  typedef Mma<T, D> X;
+  static constexpr int RPI = 64 / X::CPR, NI = R / (RPI * NW);
+  static_assert(NI * RPI * NW == R, "rows split evenly over the wavefronts");
+  static __device__ __forceinline__ int lane_offset(int k, int wave, int lane, uint32_t step) {
+    const int lrow = lane / X::CPR, r = (k * NW + wave) * RPI + lrow;
+    return (int)((uint32_t)lrow * step) + (((lane % X::CPR) ^ X::swz(r)) << 4);
+  }
+  static __device__ __forceinline__ void go(const T* base, uint32_t step, int have, uint32_t to, int wave, int lane) {
+    const uint32_t bytes = have > 0 ? (uint32_t)((have < R ? have : R) - 1) * step + X::ROWB : 0u;
+    const rsrc_words rsrc = make_rsrc(base, bytes);
+#pragma unroll
+    for (int k = 0; k < NI; ++k)
+      load_lds16(rsrc, to + (uint32_t)((k * NW + wave) * RPI * X::ROWB), lane_offset(k, wave, lane, step), (int)((uint32_t)((k * NW + wave) * RPI) * step));
+  }
+};
+// Zeros in the tile's rows that are not in `keep` (bit: row): a weight of 0 times what lies there has to be 0.
+template <typename T, int D, int NT> __device__ __forceinline__ void blank(unsigned char* tile, int R, uint64_t keep, int tid) {
+  typedef Mma<T, D> X;
+  for (int x = tid; x < R * X::CPR; x += NT)
+    if (!(keep >> (x / X::CPR) & 1u)) *reinterpret_cast<u32x4*>(tile + x * 16) = u32x4{0u, 0u, 0u, 0u};
+}
+__device__ __forceinline__ void tile_arrived() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+__device__ __forceinline__ void lds_ready() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
+
+__device__ __forceinline__ void halves(float x, float& p, float& q) {   // the values of the lane and of the one 32 apart, the lower first
+  const uint32_t u = __float_as_uint(x);
+  uint32_t u2 = u;
+  asm volatile("" : "+v"(u2));                // (two operands: with one value twice both results are taken to be equal)
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u2, false, false);
+  p = __uint_as_float(r[0]);
+  q = __uint_as_float(r[1]);
+}
+
+__device__ __forceinline__ int seen_states(const CrossArgs& a, int b) {
+  const int n = a.kv_len ? a.kv_len[b] : a.M;
+  return n < 0 ? 0 : n < a.M ? n : a.M;
+}
+// which of R keys from j0 on are seen; `byte`: the lane's byte of the mask (1 without one)
+__device__ __forceinline__ uint64_t seen_bits(int byte, int j0, int len, int R, int lane) { return __ballot(lane < R && j0 + lane < len && byte != 0); }
+__device__ __forceinline__ int mask_byte(const CrossArgs& a, int b, int j0, int len, int lane) {
+  return a.mask && j0 + lane < len ? (int)a.mask[(int64_t)b * a.M + j0 + lane] : 1;
+}
+// a register's key in a tile of 32: (v / 4) * 8 + hf * 4 + v % 4
+__device__ __forceinline__ void hide(f32x16& s, uint32_t bits, int hf) {
+  const uint32_t mine = bits >> (hf * 4);
+#pragma unroll
+  for (int v = 0; v < 16; ++v)
+    if (!(mine >> ((v >> 2) * 8 + (v & 3)) & 1u)) s[v] = -INFINITY;
+}
+
+template <typename T> constexpr int cross_keys() { return sizeof(T) == 2 ? 64 : 32; }   // keys of a tile
+
+struct CrossRow { int g, n; };
+__device__ __forceinline__ CrossRow cross_row(const CrossArgs& a, int r) {
+  if (a.group == 1) return {0, r};
+  const int g = (int)((uint32_t)r / (uint32_t)a.N);
+  return {g, r - g * a.N};
+}
+
+// 32 rows of accumulators (one in each lane) to memory through the wavefront's LDS, 16 bytes a lane: at(row) gives the row's address or null
+template <typename T, int D, typename F> __device__ __forceinline__ void rows_out(const f32x16 (&acc)[D / 32], float factor, unsigned char* mine, int lane, F&& at) {
+  typedef Mma<T, D> X;
+  const int l32 = lane & 31, hf = lane >> 5;
+#pragma unroll
+  for (int md = 0; md < D / 32; ++md)
+#pragma unroll
+    for (int g4 = 0; g4 < 4; ++g4) {
+      f32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = acc[md][g4 * 4 + e] * factor;
+      const int c = md * 32 + g4 * 8 + hf * 4, chunk = c / X::VEC;
+      unsigned char* to = mine + l32 * X::ROWB + ((chunk ^ (l32 & (X::CPR - 1))) << 4);
+      if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(to + (c % 8) * 2) = u32x2{f32_to_bf16_pair(x[0], x[1]), f32_to_bf16_pair(x[2], x[3])};
+      else *reinterpret_cast<f32x4*>(to) = x;
+    }
+  constexpr int RPI = 64 / X::CPR;
+#pragma unroll
+  for (int i = 0; i < 32 / RPI; ++i) {
+    const int row = i * RPI + lane / X::CPR, chunk = lane % X::CPR;
+    T* p = at(row);
+    if (p) *reinterpret_cast<u32x4_at2*>(p + chunk * X::VEC) = *reinterpret_cast<const u32x4*>(mine + row * X::ROWB + ((chunk ^ (row & (X::CPR - 1))) << 4));
+  }
+}
+
+template <typename T, int D, int NW, bool PART>
+__global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void cross_fwd_kernel(const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, T* __restrict__ O,
+                                                                float* __restrict__ lse, float* __restrict__ Opart, CrossArgs a) {
+  typedef Mma<T, D> X;
+  constexpr int BN = cross_keys<T>(), TILEB = BN * X::ROWB, HALVES = BN / 32;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * TILEB];   // K, V; K, V
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
+  const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int bh = blockIdx.y, b = bh / a.Hkv, hk = bh % a.Hkv, part = blockIdx.z;
+  const int row0 = (int)(blockIdx.x * (NW * 32) + wave * 32), row = row0 + l32;
+  const bool active = row < a.rows;
+  const int len = seen_states(a, b);
+  const int t0 = part * a.tiles_per_part, tiles = (len + BN - 1) / BN, t1 = t0 + a.tiles_per_part < tiles ? t0 + a.tiles_per_part : tiles;
+  const T* kb = K + b * a.k.b + hk * a.k.h;
+  const T* vb = V + b * a.v.b + hk * a.v.h;
+  const uint32_t kstep = (uint32_t)(a.k.n * (int64_t)sizeof(T)), vstep = (uint32_t)(a.v.n * (int64_t)sizeof(T));
+  const uint32_t lds = lds_address(smem);
+  auto fire = [&](int t) __attribute__((always_inline)) {
+    const uint32_t to = lds + (uint32_t)((t - t0) & 1) * 2 * TILEB;
+    Stage<T, D, BN, NW>::go(kb + (int64_t)t * BN * a.k.n, kstep, a.M - t * BN, to, wave, lane);
+    Stage<T, D, BN, NW>::go(vb + (int64_t)t * BN * a.v.n, vstep, a.M - t * BN, to + TILEB, wave, lane);
+  };
+  int byte = 1;
+  if (t0 < t1) {
+    byte = mask_byte(a, b, t0 * BN, len, lane);
+    fire(t0);
+  }
+  typename X::Frag qf[X::KS];
+  {
+    const CrossRow r = cross_row(a, row);
+    row_frags<T, D>(qf, Q + b * a.q.b + (int64_t)(hk * a.group + r.g) * a.q.h + r.n * a.q.n, hf, active);
+  }
+  f32x16 acc[X::MD];
+#pragma unroll
+  for (int md = 0; md < X::MD; ++md)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[md][v] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+  const uint32_t rbase = rows_base<T, D>(lane), cbase = X::cols_base(lane);
+  for (int t = t0; t < t1; ++t) {
+    unsigned char* tile = smem + ((t - t0) & 1) * 2 * TILEB;
+    const uint64_t seen = seen_bits(byte, t * BN, len, BN, lane);
+    tile_arrived();
+    if (t + 1 < t1) {
+      byte = mask_byte(a, b, (t + 1) * BN, len, lane);
+      fire(t + 1);
+    }
+    const bool whole = seen == (BN == 64 ? ~0ull : 0xffffffffull);
+    if (!whole) {
+      if (seen == 0) continue;
+      blank<T, D, NW * 64>(tile + TILEB, BN, seen, tid);
+      lds_ready();
+    }
+    f32x16 s[HALVES];
+#pragma unroll
+    for (int u = 0; u < HALVES; ++u) s[u] = rows<T, D>(tile + u * 32 * X::ROWB, rbase, qf);
+    if (!whole) {
+#pragma unroll
+      for (int u = 0; u < HALVES; ++u) hide(s[u], (uint32_t)(seen >> (32 * u)), hf);
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < HALVES; ++u)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) top = fmaxf(top, s[u][v]);
+    {
+      float p, q;
+      halves(top * a.scale_log2, p, q);
+      top = fmaxf(p, q);
+    }
+    const bool up = top - m_run > CROSS_LAZY;
+    if (__any(up)) {                          // (a row's own maximum decides: its bits do not depend on the rows beside it)
+      const float alpha = up ? __builtin_amdgcn_exp2f(m_run - top) : 1.f;
+      l_run *= alpha;
+#pragma unroll
+      for (int md = 0; md < X::MD; ++md)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[md][v] *= alpha;
+      m_run = up ? top : m_run;
+    }
+    const float shift = m_run == -INFINITY ? 0.f : -m_run;
+#pragma unroll
+    for (int u = 0; u < HALVES; ++u) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        s[u][v] = __builtin_amdgcn_exp2f(fmaf(s[u][v], a.scale_log2, shift));
+        l_run += s[u][v];
+      }
+      X::cols(acc, tile + TILEB + u * 32 * X::ROWB, cbase, X::weights(s[u]));
+    }
+  }
+  {
+    float p, q;
+    halves(l_run, p, q);
+    l_run = p + q;
+  }
+  const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+  const float stat = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * CROSS_LN2;
+  if constexpr (PART) {
+    if (!active) return;
+    const int64_t at = ((int64_t)part * a.B * a.Hkv + bh) * a.rows + row;
+    float* po = Opart + at * D;
+#pragma unroll
+    for (int md = 0; md < X::MD; ++md)
+#pragma unroll
+      for (int g4 = 0; g4 < 4; ++g4)
+        *reinterpret_cast<f32x4*>(po + md * 32 + g4 * 8 + hf * 4) = f32x4{acc[md][g4 * 4], acc[md][g4 * 4 + 1], acc[md][g4 * 4 + 2], acc[md][g4 * 4 + 3]} * inv;
+    if (hf == 0) lse[at] = stat;
+  } else {
+    if (lse && active && hf == 0) lse[((int64_t)b * a.Hq + hk * a.group) * a.N + row] = stat;
+    lds_ready();                              // everyone has read the last tile
+    rows_out<T, D>(acc, inv, smem + wave * 32 * X::ROWB, lane, [&](int r) __attribute__((always_inline)) -> T* {
+      if (row0 + r >= a.rows) return nullptr;
+      const CrossRow c = cross_row(a, row0 + r);
+      return O + b * a.o.b + (int64_t)(hk * a.group + c.g) * a.o.h + c.n * a.o.n;
+    });
+  }
+}
+
+// Rows of a part each -> the row: O = sum w O_part / sum w, w = exp(lse_part - their maximum).
+template <typename T, int D>
+__global__ __launch_bounds__(256) void cross_join_kernel(const float* __restrict__ Opart, const float* __restrict__ stats, T* __restrict__ O, float* __restrict__ lse, CrossArgs a) {
+  constexpr int LANES = D / 4;
+  const int64_t total = (int64_t)a.B * a.Hkv * a.rows, x = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+  if (x >= total) return;
+  const int c = threadIdx.x % LANES;
+  float top = -INFINITY;
+  for (int s = 0; s < a.parts; ++s) top = fmaxf(top, stats[s * total + x]);
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  float weight = 0.f;
+  for (int s = 0; s < a.parts; ++s) {
+    const float w = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((stats[s * total + x] - top) * CROSS_LOG2E);
+    const f32x4 o = *reinterpret_cast<const f32x4*>(Opart + (s * total + x) * D + c * 4);
+    weight += w;
+    sum += o * w;
+  }
+  const float inv = weight == 0.f ? 0.f : 1.f / weight;
+  const int bh = (int)(x / a.rows), row = (int)(x - (int64_t)bh * a.rows), b = bh / a.Hkv, hk = bh % a.Hkv;
+  const CrossRow r = cross_row(a, row);
+  Four<T>::store(O + b * a.o.b + (int64_t)(hk * a.group + r.g) * a.o.h + r.n * a.o.n + c * 4, sum * inv);
+  if (lse && c == 0) lse[((int64_t)b * a.Hq + hk * a.group) * a.N + row] = weight == 0.f ? -INFINITY : top + log2f(weight) * CROSS_LN2;
+}
+
+// dQ of 32 rows a wavefront, and D = dO.O for the kernel after it (parts: the first one's).
+template <typename T, int D, int NW, bool PART>
+__global__ __launch_bounds__(NW * 64, NW == 4 && (sizeof(T) == 2 || D == 64) ? 2 : 1) void cross_dq_kernel(const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ O,
+                                                               const float* __restrict__ lse, const T* __restrict__ dO, float* __restrict__ Dr, T* __restrict__ dQ,
+                                                               float* __restrict__ dQpart, CrossArgs a) {
+  typedef Mma<T, D> X;
+  constexpr int BN = cross_keys<T>(), TILEB = BN * X::ROWB, HALVES = BN / 32;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * TILEB];
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
+  const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int bh = blockIdx.y, b = bh / a.Hkv, hk = bh % a.Hkv, part = blockIdx.z;
+  const int row0 = (int)(blockIdx.x * (NW * 32) + wave * 32), row = row0 + l32;
+  const bool active = row < a.rows;
+  const int len = seen_states(a, b);
+  const int t0 = part * a.tiles_per_part, tiles = (len + BN - 1) / BN, t1 = t0 + a.tiles_per_part < tiles ? t0 + a.tiles_per_part : tiles;
+  const T* kb = K + b * a.k.b + hk * a.k.h;
+  const T* vb = V + b * a.v.b + hk * a.v.h;
+  const uint32_t kstep = (uint32_t)(a.k.n * (int64_t)sizeof(T)), vstep = (uint32_t)(a.v.n * (int64_t)sizeof(T));
+  const uint32_t lds = lds_address(smem);
+  auto fire = [&](int t) __attribute__((always_inline)) {
+    const uint32_t to = lds + (uint32_t)((t - t0) & 1) * 2 * TILEB;
+    Stage<T, D, BN, NW>::go(kb + (int64_t)t * BN * a.k.n, kstep, a.M - t * BN, to, wave, lane);
+    Stage<T, D, BN, NW>::go(vb + (int64_t)t * BN * a.v.n, vstep, a.M - t * BN, to + TILEB, wave, lane);
+  };
+  int byte = 1;
+  if (t0 < t1) {
+    byte = mask_byte(a, b, t0 * BN, len, lane);
+    fire(t0);
+  }
+  typename X::Frag qf[X::KS], gf[X::KS];
+  const CrossRow r = cross_row(a, row);
+  const int head = hk * a.group + r.g;
+  const int64_t stat_at = ((int64_t)b * a.Hq + hk * a.group) * a.N + row;
+  row_frags<T, D>(qf, Q + b * a.q.b + (int64_t)head * a.q.h + r.n * a.q.n, hf, active);
+  row_frags<T, D>(gf, dO + b * a.go.b + (int64_t)head * a.go.h + r.n * a.go.n, hf, active);
+  float dot = 0.f;
+  {
+    const T* op = O + b * a.o.b + (int64_t)head * a.o.h + r.n * a.o.n;
+#pragma unroll
+    for (int ks = 0; ks < X::KS; ++ks) {
+      float x[X::VEC], y[X::VEC];
+      u32x4 raw = {0u, 0u, 0u, 0u};
+      if (active) raw = *reinterpret_cast<const u32x4_at2*>(op + (2 * ks + hf) * X::VEC);
+      Elem<T>::widen(raw, x);
+      Elem<T>::widen(__builtin_bit_cast(u32x4, gf[ks]), y);
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < X::VEC; ++e) sum = fmaf(x[e], y[e], sum);
+      dot += sum;
+    }
+    float p, q;
+    halves(dot, p, q);
+    dot = p + q;
+  }
+  float shift = -INFINITY;                    // weights of 0 for a row that sees nothing
+  if (active) {
+    const float l = lse[stat_at];
+    if (l != -INFINITY) shift = -l * CROSS_LOG2E;
+    if (part == 0 && hf == 0) Dr[stat_at] = dot;
+  }
+  f32x16 acc[X::MD];
+#pragma unroll
+  for (int md = 0; md < X::MD; ++md)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[md][v] = 0.f;
+  const uint32_t rbase = rows_base<T, D>(lane), cbase = X::cols_base(lane);
+  for (int t = t0; t < t1; ++t) {
+    unsigned char* tile = smem + ((t - t0) & 1) * 2 * TILEB;
+    const uint64_t seen = seen_bits(byte, t * BN, len, BN, lane);
+    tile_arrived();
+    if (t + 1 < t1) {
+      byte = mask_byte(a, b, (t + 1) * BN, len, lane);
+      fire(t + 1);
+    }
+    const bool whole = seen == (BN == 64 ? ~0ull : 0xffffffffull);
+    if (!whole) {
+      if (seen == 0) continue;
+      blank<T, D, NW * 64>(tile, BN, seen, tid);
+      blank<T, D, NW * 64>(tile + TILEB, BN, seen, tid);
+      lds_ready();
+    }
+#pragma unroll
+    for (int u = 0; u < HALVES; ++u) {
+      const unsigned char* kt = tile + u * 32 * X::ROWB;
+      f32x16 s = rows<T, D>(kt, rbase, qf);
+      const f32x16 g = rows<T, D>(kt + TILEB, rbase, gf);
+      if (!whole) hide(s, (uint32_t)(seen >> (32 * u)), hf);
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], a.scale_log2, shift)) * (g[v] - dot);
+      X::cols(acc, kt, cbase, X::weights(s));
+    }
+  }
+  if constexpr (PART) {
+    if (!active) return;
+    float* po = dQpart + (((int64_t)part * a.B * a.Hkv + bh) * a.rows + row) * D;
+#pragma unroll
+    for (int md = 0; md < X::MD; ++md)
+#pragma unroll
+      for (int g4 = 0; g4 < 4; ++g4)
+        *reinterpret_cast<f32x4*>(po + md * 32 + g4 * 8 + hf * 4) = f32x4{acc[md][g4 * 4], acc[md][g4 * 4 + 1], acc[md][g4 * 4 + 2], acc[md][g4 * 4 + 3]};
+  } else {
+    lds_ready();
+    rows_out<T, D>(acc, a.scale, smem + wave * 32 * X::ROWB, lane, [&](int x) __attribute__((always_inline)) -> T* {
+      if (row0 + x >= a.rows) return nullptr;
+      const CrossRow c = cross_row(a, row0 + x);
+      return dQ + b * a.gq.b + (int64_t)(hk * a.group + c.g) * a.gq.h + c.n * a.gq.n;
+    });
+  }
+}
+
+// dK, dV of 32 keys a wavefront: the query rows of the key's group, a head after the other, in tiles of BN tokens.
+template <typename T, int D, bool PART>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void cross_dkv_kernel(const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const float* __restrict__ lse,
+                                                       const T* __restrict__ dO, const float* __restrict__ Dr, T* __restrict__ dK, T* __restrict__ dV,
+                                                       float* __restrict__ dKpart, float* __restrict__ dVpart, CrossArgs a) {
+  typedef Mma<T, D> X;
+  constexpr int NW = 4, BN = cross_keys<T>(), TILEB = BN * X::ROWB, OFF_STAT = 4 * TILEB, STATS = 64;   // (a load of the statistics is 64 lanes wide)
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * TILEB + 2 * 2 * STATS * 4];   // Q, dO; Q, dO; lse, D; lse, D
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int bh = blockIdx.y, b = bh / a.Hkv, hk = bh % a.Hkv, part = blockIdx.z;
+  const int key0 = (int)(blockIdx.x * (NW * 32) + wave * 32), key = key0 + l32;
+  const int len = seen_states(a, b);
+  const bool seen = key < len && (!a.mask || a.mask[(int64_t)b * a.M + key] != 0);
+  const bool any = __syncthreads_or(seen);
+  const int all = any ? a.group * a.chunks : 0;
+  const int t0 = part * a.tiles_per_part, t1 = t0 + a.tiles_per_part < all ? t0 + a.tiles_per_part : all;
+  const uint32_t qstep = (uint32_t)(a.q.n * (int64_t)sizeof(T)), gstep = (uint32_t)(a.go.n * (int64_t)sizeof(T));
+  const uint32_t lds = lds_address(smem);
+  auto fire = [&](int t) __attribute__((always_inline)) {
+    const int g = t / a.chunks, n0 = (t - g * a.chunks) * BN, head = hk * a.group + g, at = (t - t0) & 1;
+    const uint32_t to = lds + (uint32_t)at * 2 * TILEB;
+    Stage<T, D, BN, NW>::go(Q + b * a.q.b + (int64_t)head * a.q.h + (int64_t)n0 * a.q.n, qstep, a.N - n0, to, wave, lane);
+    Stage<T, D, BN, NW>::go(dO + b * a.go.b + (int64_t)head * a.go.h + (int64_t)n0 * a.go.n, gstep, a.N - n0, to + TILEB, wave, lane);
+    if (wave < 2) {
+      const float* from = (wave ? Dr : lse) + ((int64_t)b * a.Hq + head) * a.N + n0;
+      const int have = a.N - n0 < BN ? a.N - n0 : BN;
+      const rsrc_words rsrc = make_rsrc(from, (uint32_t)have * 4);
+      load_lds4(rsrc, lds + (uint32_t)(OFF_STAT + (at * 2 + wave) * STATS * 4), lane * 4, 0);
+    }
+  };
+  if (t0 < t1) fire(t0);
+  typename X::Frag kf[X::KS], vf[X::KS];
+  row_frags<T, D>(kf, K + b * a.k.b + hk * a.k.h + key * a.k.n, hf, seen);
+  row_frags<T, D>(vf, V + b * a.v.b + hk * a.v.h + key * a.v.n, hf, seen);
+  f32x16 dk[X::MD], dv[X::MD];
+#pragma unroll
+  for (int md = 0; md < X::MD; ++md)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) dk[md][v] = dv[md][v] = 0.f;
+  const uint32_t rbase = rows_base<T, D>(lane), cbase = X::cols_base(lane);
+  for (int t = t0; t < t1; ++t) {
+    const int at = (t - t0) & 1, have = a.N - t % a.chunks * BN;
+    unsigned char* tile = smem + at * 2 * TILEB;
+    float* stat = reinterpret_cast<float*>(smem + OFF_STAT + at * 2 * STATS * 4);
+    tile_arrived();
+    if (t + 1 < t1) fire(t + 1);
+    if (have < BN) {
+      const uint64_t keep = (1ull << have) - 1ull;
+      blank<T, D, 256>(tile, BN, keep, tid);
+      blank<T, D, 256>(tile + TILEB, BN, keep, tid);
+      if (tid < BN && tid >= have) {
+        stat[tid] = INFINITY;
+        stat[STATS + tid] = 0.f;
+      }
+      lds_ready();
+    }
+#pragma unroll
+    for (int u = 0; u < BN / 32; ++u) {
+      const unsigned char* qt = tile + u * 32 * X::ROWB;
+      f32x16 s = rows<T, D>(qt, rbase, kf), g = rows<T, D>(qt + TILEB, rbase, vf);
+#pragma unroll
+      for (int g4 = 0; g4 < 4; ++g4) {
+        const f32x4 l = *reinterpret_cast<const f32x4*>(stat + u * 32 + g4 * 8 + hf * 4), d = *reinterpret_cast<const f32x4*>(stat + STATS + u * 32 + g4 * 8 + hf * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int v = g4 * 4 + e;
+          s[v] = l[e] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[v], a.scale_log2, -l[e] * CROSS_LOG2E));
+          g[v] = s[v] * (g[v] - d[e]);
+        }
+      }
+      X::cols(dv, qt + TILEB, cbase, X::weights(s));
+      X::cols(dk, qt, cbase, X::weights(g));
+    }
+  }
+  if constexpr (PART) {
+    if (key >= a.M) return;
+    const int64_t to = (((int64_t)part * a.B * a.Hkv + bh) * a.M + key) * D;
+#pragma unroll
+    for (int md = 0; md < X::MD; ++md)
+#pragma unroll
+      for (int g4 = 0; g4 < 4; ++g4) {
+        const int c = md * 32 + g4 * 8 + hf * 4;
+        f32x4 x, y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[e] = seen ? dk[md][g4 * 4 + e] : 0.f;
+          y[e] = seen ? dv[md][g4 * 4 + e] : 0.f;
+        }
+        *reinterpret_cast<f32x4*>(dKpart + to + c) = x;
+        *reinterpret_cast<f32x4*>(dVpart + to + c) = y;
+      }
+  } else {
+    if (!seen) {
+#pragma unroll
+      for (int md = 0; md < X::MD; ++md)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) dk[md][v] = dv[md][v] = 0.f;
+    }
+    lds_ready();
+    unsigned char* mine = smem + wave * 32 * X::ROWB;
+    rows_out<T, D>(dk, a.scale, mine, lane, [&](int x) __attribute__((always_inline)) -> T* {
+      return key0 + x < a.M ? dK + b * a.gk.b + hk * a.gk.h + (int64_t)(key0 + x) * a.gk.n : nullptr;
+    });
+    rows_out<T, D>(dv, 1.f, mine, lane, [&](int x) __attribute__((always_inline)) -> T* {
+      return key0 + x < a.M ? dV + b * a.gv.b + hk * a.gv.h + (int64_t)(key0 + x) * a.gv.n : nullptr;
+    });
+  }
+}
+
+// out[b, h, l, :] = factor * sum over the parts, in their order
+template <typename T, int D>
+__global__ __launch_bounds__(256) void cross_sum_kernel(const float* __restrict__ part, T* __restrict__ out, int H, int L, int64_t total, int parts, float factor, Strides to) {
+  constexpr int LANES = D / 4;
+  const int64_t x = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+  if (x >= total) return;
+  const int c = threadIdx.x % LANES;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < parts; ++s) sum += *reinterpret_cast<const f32x4*>(part + (s * total + x) * D + c * 4);
+  const int64_t bh = x / L;
+  Four<T>::store(out + bh / H * to.b + bh % H * to.h + (x - bh * L) * to.n + c * 4, sum * factor);
+}
+
+// ---- host
+
+// Wavefronts of a workgroup by the rows that a key head has: no more than have rows.
+static int cross_waves(const Plan& pl) {
+  const int64_t rows = (int64_t)pl.group * pl.N;
+  return rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+}
+static int cross_tile(const Plan& pl) { return pl.dtype == PSA_BF16 ? cross_keys<bf16_t>() : cross_keys<float>(); }
+// Workgroups that share the keys of a block of rows, where there are too few blocks to fill the chip: each at least four tiles.
+int cross_key_parts(const Plan& pl, int M) {
+  const int64_t rows = (int64_t)pl.group * pl.N, per = cross_waves(pl) * 32, blocks = (rows + per - 1) / per * pl.B * pl.Hkv;
+  const int tiles = (M + cross_tile(pl) - 1) / cross_tile(pl);
+  int64_t parts = 512 / blocks, most = tiles / 4;
+  parts = parts < most ? parts : most;
+  return parts < 1 ? 1 : (int)parts;
+}
+// Workgroups that share the rows of a block of 128 keys: each at least eight tiles.
+int cross_row_parts(const Plan& pl, int M) {
+  const int64_t blocks = (int64_t)(M + 127) / 128 * pl.B * pl.Hkv;
+  if (blocks == 0) return 1;
+  const int64_t tiles = (int64_t)pl.group * ((pl.N + cross_tile(pl) - 1) / cross_tile(pl));
+  int64_t parts = 512 / blocks, most = tiles / 8;
+  parts = parts < most ? parts : most;
+  return parts < 1 ? 1 : (int)parts;
+}
+
+static CrossArgs cross_args(const Plan& pl, const CrossCall& c) {
+  CrossArgs a;
+  a.B = pl.B; a.Hq = pl.Hq; a.Hkv = pl.Hkv; a.group = pl.group; a.N = pl.N; a.M = c.M; a.rows = pl.group * pl.N;
+  a.scale = pl.scale; a.scale_log2 = pl.scale * CROSS_LOG2E;
+  a.q = c.q; a.k = c.k; a.v = c.v; a.o = c.o; a.gq = c.gq; a.gk = c.gk; a.gv = c.gv; a.go = c.go;
+  a.kv_len = c.kv_len; a.mask = c.key_mask;
+  a.chunks = (pl.N + cross_tile(pl) - 1) / cross_tile(pl);
+  return a;
+}
+static void cross_share(CrossArgs& a, int parts, int tiles) {
+  a.parts = parts;
+  a.tiles_per_part = parts > 0 ? (tiles + parts - 1) / parts : tiles;
+}
+
+template <typename T, int D>
+static void launch_cross_fwd_t(const Plan& pl, const CrossCall& c, const void* Q, const void* K, const void* V, void* O, float* lse, float* part, float* stats, hipStream_t s) {
+  CrossArgs a = cross_args(pl, c);
+  const int nw = cross_waves(pl);
+  cross_share(a, cross_key_parts(pl, c.M), (c.M + cross_keys<T>() - 1) / cross_keys<T>());
+  const dim3 grid((unsigned)((a.rows + nw * 32 - 1) / (nw * 32)), (unsigned)(pl.B * pl.Hkv), (unsigned)a.parts);
+  const bool split = a.parts > 1;
+  auto go = [&](auto kernel) {
+    kernel<<<grid, nw * 64, 0, s>>>(static_cast<const T*>(Q), static_cast<const T*>(K), static_cast<const T*>(V), static_cast<T*>(O), split ? stats : lse, part, a);
+  };
+  if (nw == 1) split ? go(cross_fwd_kernel<T, D, 1, true>) : go(cross_fwd_kernel<T, D, 1, false>);
+  else if (nw == 2) split ? go(cross_fwd_kernel<T, D, 2, true>) : go(cross_fwd_kernel<T, D, 2, false>);
+  else split ? go(cross_fwd_kernel<T, D, 4, true>) : go(cross_fwd_kernel<T, D, 4, false>);
+  if (!split) return;
+  const int64_t total = (int64_t)pl.B * pl.Hq * pl.N, per = 256 / (D / 4);
+  cross_join_kernel<T, D><<<(unsigned)((total + per - 1) / per), 256, 0, s>>>(part, stats, static_cast<T*>(O), lse, a);
+}
+
+hipError_t launch_cross_fwd(const Plan& pl, const CrossCall& c, const void* Q, const void* K, const void* V, void* O, float* lse, float* part, float* stats, hipStream_t s) {
+  if (pl.dtype == PSA_BF16) pl.d == 128 ? launch_cross_fwd_t<bf16_t, 128>(pl, c, Q, K, V, O, lse, part, stats, s) : launch_cross_fwd_t<bf16_t, 64>(pl, c, Q, K, V, O, lse, part, stats, s);
+  else pl.d == 128 ? launch_cross_fwd_t<float, 128>(pl, c, Q, K, V, O, lse, part, stats, s) : launch_cross_fwd_t<float, 64>(pl, c, Q, K, V, O, lse, part, stats, s);
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+static void launch_cross_bwd_t(const Plan& pl, const CrossCall& c, const void* Q, const void* K, const void* V, const void* O, const float* lse, const void* dO, void* dQ, void* dK,
+                               void* dV, float* Dr, float* dQpart, float* dKpart, float* dVpart, hipStream_t s) {
+  CrossArgs a = cross_args(pl, c);
+  const T *q = static_cast<const T*>(Q), *k = static_cast<const T*>(K), *v = static_cast<const T*>(V), *o = static_cast<const T*>(O), *g = static_cast<const T*>(dO);
+  const int nw = cross_waves(pl), per = 256 / (D / 4);
+  cross_share(a, cross_key_parts(pl, c.M), (c.M + cross_keys<T>() - 1) / cross_keys<T>());
+  {
+    const dim3 grid((unsigned)((a.rows + nw * 32 - 1) / (nw * 32)), (unsigned)(pl.B * pl.Hkv), (unsigned)a.parts);
+    const bool split = a.parts > 1;
+    auto go = [&](auto kernel) { kernel<<<grid, nw * 64, 0, s>>>(q, k, v, o, lse, g, Dr, static_cast<T*>(dQ), dQpart, a); };
+    if (nw == 1) split ? go(cross_dq_kernel<T, D, 1, true>) : go(cross_dq_kernel<T, D, 1, false>);
+    else if (nw == 2) split ? go(cross_dq_kernel<T, D, 2, true>) : go(cross_dq_kernel<T, D, 2, false>);
+    else split ? go(cross_dq_kernel<T, D, 4, true>) : go(cross_dq_kernel<T, D, 4, false>);
+    const int64_t total = (int64_t)pl.B * pl.Hq * pl.N;
+    if (split) cross_sum_kernel<T, D><<<(unsigned)((total + per - 1) / per), 256, 0, s>>>(dQpart, static_cast<T*>(dQ), pl.Hq, pl.N, total, a.parts, pl.scale, c.gq);
+  }
+  if (c.M == 0) return;
+  cross_share(a, cross_row_parts(pl, c.M), pl.group * a.chunks);
+  const dim3 grid((unsigned)((c.M + 127) / 128), (unsigned)(pl.B * pl.Hkv), (unsigned)a.parts);
+  auto go = [&](auto kernel) { kernel<<<grid, 256, 0, s>>>(q, k, v, lse, g, Dr, static_cast<T*>(dK), static_cast<T*>(dV), dKpart, dVpart, a); };
+  if (a.parts > 1) {
+    go(cross_dkv_kernel<T, D, true>);
+    const int64_t total = (int64_t)pl.B * pl.Hkv * c.M;
+    const unsigned n = (unsigned)((total + per - 1) / per);
+    cross_sum_kernel<T, D><<<n, 256, 0, s>>>(dKpart, static_cast<T*>(dK), pl.Hkv, c.M, total, a.parts, pl.scale, c.gk);
+    cross_sum_kernel<T, D><<<n, 256, 0, s>>>(dVpart, static_cast<T*>(dV), pl.Hkv, c.M, total, a.parts, 1.f, c.gv);
+  } else {
+    go(cross_dkv_kernel<T, D, false>);
+  }
+}
+
+hipError_t launch_cross_bwd(const Plan& pl, const CrossCall& c, const void* Q, const void* K, const void* V, const void* O, const float* lse, const void* dO, void* dQ, void* dK,
+                            void* dV, float* Dr, float* dQpart, float* dKpart, float* dVpart, hipStream_t s) {
+  auto go = [&](auto f) { f(pl, c, Q, K, V, O, lse, dO, dQ, dK, dV, Dr, dQpart, dKpart, dVpart, s); };
+  if (pl.dtype == PSA_BF16) pl.d == 128 ? go(launch_cross_bwd_t<bf16_t, 128>) : go(launch_cross_bwd_t<bf16_t, 64>);
+  else pl.d == 128 ? go(launch_cross_bwd_t<float, 128>) : go(launch_cross_bwd_t<float, 64>);
+  return hipGetLastError();
+}
+
+}  // namespace psa

@@ -121,6 +121,29 @@ template <int D> __host__ __device__ constexpr int row_swizzle32(int row) {
   return D == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
 }
 
+typedef __attribute__((ext_vector_type(4))) uint32_t rsrc_words;
+// Loads straight into LDS, at `to` + lane * (16 or 4): source = buffer + v + s.  In assembly, so that the compiler does not track them:
+// next to LDS reads it would make each of those wait for every load in flight, also for those into the other buffer.  They
+// are waited for by hand (vmcnt) before the barrier behind which their bytes are read.
+// (m0 is a reserved register: the compiler keeps nothing in it and warns that it would not restore it.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void load_lds16(const rsrc_words& rsrc, uint32_t to, int v, int s) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(v), "s"(rsrc), "s"(s) : "memory", "m0");
+}
+__device__ __forceinline__ void load_lds4(const rsrc_words& rsrc, uint32_t to, int v, int s) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(to), "v"(v), "s"(rsrc), "s"(s) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+// buffer descriptor: base, bytes, 32-bit data format
+__device__ __forceinline__ rsrc_words make_rsrc(const void* base, uint32_t bytes) {
+  const uint64_t at = (uint64_t)base;
+  rsrc_words r = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, bytes, 0x00020000u};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = (uint32_t)__builtin_amdgcn_readfirstlane((int)r[i]);
+  return r;
+}
+
 // float32 on the bfloat16 matrix cores: x = h + m + l exactly, three bfloat16 (8 bits each, the remainders rounded to nearest and signed), so that
 // a product is the six terms down to 2^-16 of it (h h, h m, m h, m m, h l, l h); the three that are left out are of the order of 2^-25 of it.
 // Not for values that are not finite (or round to infinity): their m and l are NaN.  Nor for those whose last bits lie below 2^-133, the smallest

@@ -70,6 +70,19 @@ constexpr int ROTARY_PAIRS = 64;
 hipError_t launch_rotary(const Plan& pl, const psa_rotary_spec& r, int Hq, int Hkv, const Strides& q, const Strides& k, const int32_t* pos, int64_t pos_stride,
                          const int32_t* perm, bool inverse, const void* Qin, const void* Kin, void* Qout, void* Kout, hipStream_t s);
 void rotary_spectrum_host(int d, int axes, const int32_t* pairs, double base, bool shared, psa_rotary_spec* r);
+// Cross attention to M states.  part, stats / dQpart / dKpart, dVpart: partial results in fp32 (cross_key_parts or cross_row_parts times the
+// result's elements; unused where that is 1); Dr: a float per query row.
+struct CrossCall {
+  int M;
+  Strides q, k, v, o, gq, gk, gv, go;         // g: the gradients
+  const int32_t* kv_len;
+  const uint8_t* key_mask;
+};
+int cross_key_parts(const Plan& pl, int M);
+int cross_row_parts(const Plan& pl, int M);
+hipError_t launch_cross_fwd(const Plan& pl, const CrossCall& c, const void* Q, const void* K, const void* V, void* O, float* lse, float* part, float* stats, hipStream_t s);
+hipError_t launch_cross_bwd(const Plan& pl, const CrossCall& c, const void* Q, const void* K, const void* V, const void* O, const float* lse, const void* dO, void* dQ, void* dK,
+                            void* dV, float* Dr, float* dQpart, float* dKpart, float* dVpart, hipStream_t s);
 // Rk (nullable): also the keys'
 hipError_t launch_representatives(const Plan& pl, const void* Q, void* Rq, const void* K, void* Rk, hipStream_t s);
 // part: per (row, key slice) partial softmax statistics of the matrix-core path (Plan::off_part)
