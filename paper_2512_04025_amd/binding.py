@@ -46,17 +46,34 @@ class PsaParams(ctypes.Structure):
         return -(-self.N // self.bk)
 
 
+def _stride_field(name: str):
+    """A spec's strides as a tuple: kept beside the struct's words, since every call compares them with its tensors."""
+    words, kept = "_" + name, "_" + name + "_tuple"
+
+    def get(self):
+        return getattr(self, kept, (0, 0, 0))
+
+    def put(self, strides):
+        b, h, n = (int(s) for s in strides)
+        setattr(self, words, (b, h, n))
+        setattr(self, kept, (b, h, n))
+    return property(get, put)
+
+
 class PsaRotary(ctypes.Structure):
     """Mirror of `psa_rotary_spec` in include/psa.h (see make_rotary)."""
     _fields_ = [
         ("axes", ctypes.c_int32), ("pairing", ctypes.c_int32), ("axis", ctypes.c_uint8 * 64), ("freq", ctypes.c_double * 64),
-        ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3),
+        ("_q_stride", ctypes.c_int64 * 3), ("_k_stride", ctypes.c_int64 * 3),
     ]
+    q_stride, k_stride = _stride_field("q_stride"), _stride_field("k_stride")
 
 
 class PsaCross(ctypes.Structure):
     """Mirror of `psa_cross` in include/psa.h (see make_cross)."""
-    _fields_ = [("M", ctypes.c_int32)] + [(n + "_stride", ctypes.c_int64 * 3) for n in ("q", "k", "v", "o", "dq", "dk", "dv", "do")]
+    _fields_ = [("M", ctypes.c_int32)] + [("_" + n + "_stride", ctypes.c_int64 * 3) for n in ("q", "k", "v", "o", "dq", "dk", "dv", "do")]
+    q_stride, k_stride, v_stride, o_stride = (_stride_field(n + "_stride") for n in "qkvo")
+    dq_stride, dk_stride, dv_stride, do_stride = (_stride_field("d" + n + "_stride") for n in "qkvo")
 
 
 def library_path() -> str:
@@ -189,41 +206,45 @@ def _strides_of(x) -> Tuple[int, int, int]:
     return (0, 0, 0) if x.is_contiguous() else tuple(x.stride()[:3])
 
 
-def _dtype_of(p: PsaParams):
-    import torch
-    return torch.bfloat16 if p.dtype == PSA_BF16 else torch.float32
+_CONTIGUOUS = (0, 0, 0)
 
 
-def _rows(x, shape, dtype, strides, device):
+def _rows(x, shape, dtype, strides, device: int):
     """Device pointer of a [B, H, L, d] tensor that the kernels address by `strides` ((0, 0, 0): contiguous)."""
     if x is None:
         return None
     if x.shape != shape or x.dtype != dtype:
         raise ValueError(f"expected a {dtype} tensor of shape {tuple(shape)}, got {x.dtype} {tuple(x.shape)}")
-    if x.device != device:
+    if x.get_device() != device:
         raise ValueError("libpsa takes tensors of the current device")
-    if strides == (0, 0, 0):
+    if strides == _CONTIGUOUS:
         if not x.is_contiguous():
             raise ValueError("the tensor is not contiguous: give its strides to the spec")
-    elif x.numel():
+    elif x.stride() != strides + (1,) and x.numel():
         for n, want, got in zip(shape, strides + (1,), x.stride()):
             if n > 1 and want != got:
                 raise ValueError(f"the tensor's strides {x.stride()} are not the spec's {strides}")
     return x.data_ptr()
 
 
-def _table(x, shapes, dtype, device, what):
+def _table(x, shapes, dtype, device: int, what):
     """Device pointer of a contiguous table (None stays NULL)."""
     if x is None:
         return None
-    if x.dtype != dtype or tuple(x.shape) not in shapes or x.device != device or not x.is_contiguous():
+    if x.dtype != dtype or x.shape not in shapes or x.get_device() != device or not x.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous {dtype} tensor of shape {' or '.join(map(str, shapes))} on the current device")
     return x.data_ptr()
 
 
-def _here():
+def _here(p: PsaParams, stream):
+    """The library, torch, the current device, its stream to work on, p's element type."""
     import torch
-    return torch.device("cuda", torch.cuda.current_device())
+    dev = torch.cuda.current_device()
+    if stream is None:
+        stream = torch._C._cuda_getCurrentRawStream(dev)
+    else:
+        stream = getattr(stream, "cuda_stream", stream)
+    return _lib or load_library(), torch, dev, stream or None, torch.bfloat16 if p.dtype == PSA_BF16 else torch.float32
 
 
 def make_rotary(d: int, pairs: Sequence[int], base: float = 10000.0, shared: bool = False, pairing: int = PSA_ROTARY_ADJACENT,
@@ -240,19 +261,21 @@ def make_rotary(d: int, pairs: Sequence[int], base: float = 10000.0, shared: boo
 
 def psa_rotary(p: PsaParams, r: PsaRotary, pos, Qin, Kin, Qout, Kout, perm=None, inverse: bool = False, stream=None) -> None:
     """Q and K ([B, heads, N, d], either may be None on both sides) turned by pos (int32 [axes, N], [1, axes, N] or [B, axes, N])."""
-    import torch
-    dev, dt = _here(), _dtype_of(p)
-    q, k, tight = tuple(r.q_stride), tuple(r.k_stride), (0, 0, 0)
-    sq, sk = (p.B, p.Hq, p.N, p.d), (p.B, p.Hkv, p.N, p.d)
-    shapes = ((r.axes, p.N), (1, r.axes, p.N), (p.B, r.axes, p.N))
-    at = _table(pos, shapes, torch.int32, dev, "pos")
-    if at is None:
+    lib, torch, dev, at, dt = _here(p, stream)
+    B, N, axes = p.B, p.N, r.axes
+    sq, sk = (B, p.Hq, N, p.d), (B, p.Hkv, N, p.d)
+    if pos is None:
         raise ValueError("pos is needed")
-    _check(load_library().psa_rotary(
-        ctypes.byref(p), ctypes.byref(r), at, r.axes * p.N if pos.dim() == 3 and pos.shape[0] > 1 else 0,
-        _table(perm, ((p.N,),), torch.int32, dev, "perm"), 1 if inverse else 0,
-        _rows(Qin, sq, dt, tight if inverse else q, dev), _rows(Kin, sk, dt, tight if inverse else k, dev),
-        _rows(Qout, sq, dt, q if inverse else tight, dev), _rows(Kout, sk, dt, k if inverse else tight, dev), _stream(stream)), "psa_rotary")
+    loose_q, loose_k, tight = r.q_stride, r.k_stride, _CONTIGUOUS
+    if inverse:
+        q, k, qo, ko = _rows(Qin, sq, dt, tight, dev), _rows(Kin, sk, dt, tight, dev), _rows(Qout, sq, dt, loose_q, dev), _rows(Kout, sk, dt, loose_k, dev)
+    else:
+        q, k, qo, ko = _rows(Qin, sq, dt, loose_q, dev), _rows(Kin, sk, dt, loose_k, dev), _rows(Qout, sq, dt, tight, dev), _rows(Kout, sk, dt, tight, dev)
+    status = lib.psa_rotary(
+        ctypes.byref(p), ctypes.byref(r), _table(pos, ((axes, N), (1, axes, N), (B, axes, N)), torch.int32, dev, "pos"),
+        axes * N if pos.dim() == 3 and pos.shape[0] > 1 else 0, _table(perm, ((N,),), torch.int32, dev, "perm"), 1 if inverse else 0, q, k, qo, ko, at)
+    if status:
+        raise PsaError(status, "psa_rotary")
 
 
 def _thresholds(p: PsaParams, tau_s: Sequence[float]):
@@ -328,44 +351,51 @@ def psa_query_cross_sizes(p: PsaParams, x) -> Tuple[int, int]:
     return fwd.value, bwd.value
 
 
-def _scratch(p: PsaParams, x: PsaCross, scratch, which: int, device):
+def _scratch(lib, p: PsaParams, x: PsaCross, scratch, backward: bool, device: int):
     """Device pointer of a workspace that is large enough."""
-    need = psa_query_cross_sizes(p, x)[which]
+    need = ctypes.c_size_t(0)
+    status = lib.psa_query_cross_sizes(ctypes.byref(p), ctypes.byref(x), None if backward else ctypes.byref(need), ctypes.byref(need) if backward else None)
+    if status:
+        raise PsaError(status, "psa_query_cross_sizes")
     if scratch is None:
-        if need:
-            raise ValueError(f"{need} bytes of scratch are needed")
+        if need.value:
+            raise ValueError(f"{need.value} bytes of scratch are needed")
         return None
-    if scratch.device != device or not scratch.is_contiguous() or scratch.numel() * scratch.element_size() < need:
-        raise ValueError(f"scratch: a contiguous tensor of {need} bytes on the current device is needed")
+    if scratch.get_device() != device or not scratch.is_contiguous() or scratch.numel() * scratch.element_size() < need.value:
+        raise ValueError(f"scratch: a contiguous tensor of {need.value} bytes on the current device is needed")
     return scratch.data_ptr()
+
+
+def _seen(torch, p: PsaParams, x: PsaCross, kv_len, key_mask, device: int):
+    """Device pointers of the lengths and the mask."""
+    return (_table(kv_len, ((p.B,),), torch.int32, device, "kv_len"),
+            None if key_mask is None else _table(key_mask, ((p.B, x.M),), torch.bool if key_mask.dtype == torch.bool else torch.uint8, device, "key_mask"))
 
 
 def psa_cross_attention_fwd(p: PsaParams, x: PsaCross, Q, K, V, O, scratch=None, lse=None, kv_len=None, key_mask=None, stream=None) -> None:
     """Q, O: [B, Hq, N, d]; K, V: [B, Hkv, M, d]; kv_len: int32 [B]; key_mask: uint8 or bool [B, M]; lse: float [B, Hq, N]."""
-    import torch
-    dev, dt = _here(), _dtype_of(p)
-    sq, sk = (p.B, p.Hq, p.N, p.d), (p.B, p.Hkv, x.M, p.d)
-    _check(load_library().psa_cross_attention_fwd(
-        ctypes.byref(p), ctypes.byref(x), _rows(Q, sq, dt, tuple(x.q_stride), dev), _rows(K, sk, dt, tuple(x.k_stride), dev), _rows(V, sk, dt, tuple(x.v_stride), dev),
-        _table(kv_len, ((p.B,),), torch.int32, dev, "kv_len"), _mask(p, x, key_mask, dev), _rows(O, sq, dt, tuple(x.o_stride), dev),
-        _table(lse, ((p.B, p.Hq, p.N),), torch.float32, dev, "lse"), _scratch(p, x, scratch, 0, dev), _stream(stream)), "psa_cross_attention_fwd")
-
-
-def _mask(p: PsaParams, x: PsaCross, key_mask, device):
-    import torch
-    return None if key_mask is None else _table(key_mask, ((p.B, x.M),), torch.bool if key_mask.dtype == torch.bool else torch.uint8, device, "key_mask")
+    lib, torch, dev, at, dt = _here(p, stream)
+    B, Hq, N, d = p.B, p.Hq, p.N, p.d
+    sq, sk = (B, Hq, N, d), (B, p.Hkv, x.M, d)
+    status = lib.psa_cross_attention_fwd(
+        ctypes.byref(p), ctypes.byref(x), _rows(Q, sq, dt, x.q_stride, dev), _rows(K, sk, dt, x.k_stride, dev), _rows(V, sk, dt, x.v_stride, dev),
+        *_seen(torch, p, x, kv_len, key_mask, dev), _rows(O, sq, dt, x.o_stride, dev), _table(lse, ((B, Hq, N),), torch.float32, dev, "lse"),
+        _scratch(lib, p, x, scratch, False, dev), at)
+    if status:
+        raise PsaError(status, "psa_cross_attention_fwd")
 
 
 def psa_cross_attention_bwd(p: PsaParams, x: PsaCross, Q, K, V, O, lse, dO, dQ, dK, dV, scratch, kv_len=None, key_mask=None, stream=None) -> None:
-    import torch
-    dev, dt = _here(), _dtype_of(p)
-    sq, sk = (p.B, p.Hq, p.N, p.d), (p.B, p.Hkv, x.M, p.d)
-    rows = lambda t, s, name: _rows(t, s, dt, tuple(getattr(x, name)), dev)          # noqa: E731
-    _check(load_library().psa_cross_attention_bwd(
-        ctypes.byref(p), ctypes.byref(x), rows(Q, sq, "q_stride"), rows(K, sk, "k_stride"), rows(V, sk, "v_stride"),
-        _table(kv_len, ((p.B,),), torch.int32, dev, "kv_len"), _mask(p, x, key_mask, dev), rows(O, sq, "o_stride"), _table(lse, ((p.B, p.Hq, p.N),), torch.float32, dev, "lse"),
-        rows(dO, sq, "do_stride"), rows(dQ, sq, "dq_stride"), rows(dK, sk, "dk_stride"), rows(dV, sk, "dv_stride"), _scratch(p, x, scratch, 1, dev), _stream(stream)),
-        "psa_cross_attention_bwd")
+    lib, torch, dev, at, dt = _here(p, stream)
+    B, Hq, N, d = p.B, p.Hq, p.N, p.d
+    sq, sk = (B, Hq, N, d), (B, p.Hkv, x.M, d)
+    status = lib.psa_cross_attention_bwd(
+        ctypes.byref(p), ctypes.byref(x), _rows(Q, sq, dt, x.q_stride, dev), _rows(K, sk, dt, x.k_stride, dev), _rows(V, sk, dt, x.v_stride, dev),
+        *_seen(torch, p, x, kv_len, key_mask, dev), _rows(O, sq, dt, x.o_stride, dev), _table(lse, ((B, Hq, N),), torch.float32, dev, "lse"),
+        _rows(dO, sq, dt, x.do_stride, dev), _rows(dQ, sq, dt, x.dq_stride, dev), _rows(dK, sk, dt, x.dk_stride, dev), _rows(dV, sk, dt, x.dv_stride, dev),
+        _scratch(lib, p, x, scratch, True, dev), at)
+    if status:
+        raise PsaError(status, "psa_cross_attention_bwd")
 
 
 def psa_probe_copy(src, dst, nbytes: int, stream=None) -> None:
