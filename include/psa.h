@@ -301,8 +301,8 @@ int psa_dense_ref(const psa_params* p, const void* Q, const void* K, const void*
  *
  * psa_cross: M, and per tensor the elements from one batch entry, head, token (state) to the next; channels are adjacent; all three 0:
  *   contiguous [B, heads, N or M, d].  Not negative.  Inputs may repeat rows (stride 0, states that a batch shares); tensors that are written
- *   may not: ordered by size, each stride must reach past what the smaller ones cover.  From one state to the next at most 32 MB (backward:
- *   tokens of Q and dO too).  The d*_stride are read by the backward call only, do_stride is dO's.
+ *   may not: ordered by size, each stride must reach past what the smaller ones cover.  From one token or state to the next at most
+ *   32 MB.  The d*_stride are read by the backward call only, do_stride is dO's.
  *   M = 0 is allowed (K, V, dK, dV may then be NULL).
  * psa_query_cross_sizes (host call): bytes of workspace, either pointer may be NULL.  0 for most forward calls: only where few query
  *   rows meet many states do workgroups share a row's states and leave partial results there.  256-byte aligned.

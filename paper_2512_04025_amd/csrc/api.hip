@@ -438,7 +438,8 @@ static int make_cross(const psa_params* p, const psa_cross* x, Plan* pl, CrossCa
                     !make_strides(x->dk_stride, B, Hkv, M, d, true, &c->gk) || !make_strides(x->dv_stride, B, Hkv, M, d, true, &c->gv))) return PSA_EINVAL;
   // offsets inside a tile of 64 rows are 32 bits wide, and so are the rows of a key head
   const int64_t most = ((int64_t)1 << 25) / pl->esize;
-  if (c->k.n >= most || c->v.n >= most || (gradients && (c->q.n >= most || c->go.n >= most))) return PSA_EUNSUPPORTED;
+  if (c->k.n >= most || c->v.n >= most || c->q.n >= most || c->o.n >= most) return PSA_EUNSUPPORTED;
+  if (gradients && (c->go.n >= most || c->gq.n >= most)) return PSA_EUNSUPPORTED;
   if ((int64_t)B * Hkv > 65535 || (int64_t)pl->group * N > 0x7fffffff - 128 || M > 0x7fffffff - 128) return PSA_EUNSUPPORTED;
   return PSA_OK;
 }

@@ -17,6 +17,7 @@ namespace psa {
 struct CrossArgs {
   int B, Hq, Hkv, group, N, M;
   int rows;                                   // group * N: query rows of a key head
+  int flat;                                   // a block of rows may hold rows of several heads
   int parts, tiles_per_part;                  // workgroups that share a row's keys (forward, dQ) or a key's rows (dK, dV)
   int chunks;                                 // dK, dV: tiles of one head's tokens
   float scale, scale_log2;
@@ -185,6 +186,33 @@ __device__ __forceinline__ CrossRow cross_row(const CrossArgs& a, int r) {
   return {g, r - g * a.N};
 }
 
+// Tiles of consecutive rows, one after the other, straight into LDS: what is fixed is made once.
+template <typename T, int D, int R, int NW> struct TileStream {
+  typedef Mma<T, D> X;
+  static constexpr int RPI = 64 / X::CPR, NI = R / (RPI * NW), OFFS = (16 / RPI + NW - 1) / NW;   // (the permutation of the chunks has period 16)
+  uint64_t base;
+  uint32_t step;                              // bytes from one row to the next
+  int left;                                   // rows from the next tile's first on
+  int off[OFFS];
+  __device__ __forceinline__ TileStream(const T* from, uint32_t step_, int left_, int wave, int lane) : base((uint64_t)from), step(step_), left(left_) {
+#pragma unroll
+    for (int k = 0; k < OFFS; ++k) off[k] = Stage<T, D, R, NW>::lane_offset(k, wave, lane, step);
+  }
+  __device__ __forceinline__ void next(uint32_t to, int wave) {       // `left` > 0
+    const rsrc_words rsrc = make_rsrc((const void*)base, (uint32_t)((left < R ? left : R) - 1) * step + X::ROWB);
+#pragma unroll
+    for (int k = 0; k < NI; ++k)
+      load_lds16(rsrc, to + (uint32_t)((k * NW + wave) * RPI * X::ROWB), off[k % OFFS], (int)((uint32_t)((k * NW + wave) * RPI) * step));
+    base += (uint64_t)R * step;
+    left -= R;
+  }
+};
+
+// 32 rows of one head, a row in each lane, through a buffer descriptor whose range ends with the head's rows: rows behind it are read as zeros and not written.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const void* base, uint32_t step, int have, int rowb) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, have > 0 ? (int)((uint32_t)((have < 32 ? have : 32) - 1) * step + (uint32_t)rowb) : 0, 0x00020000);
+}
+
 // 32 rows of accumulators (one in each lane) to memory through the wavefront's LDS, 16 bytes a lane: at(row) gives the row's address or null
 template <typename T, int D, typename F> __device__ __forceinline__ void rows_out(const f32x16 (&acc)[D / 32], float factor, unsigned char* mine, int lane, F&& at) {
   typedef Mma<T, D> X;
@@ -207,6 +235,63 @@ template <typename T, int D, typename F> __device__ __forceinline__ void rows_ou
     const int row = i * RPI + lane / X::CPR, chunk = lane % X::CPR;
     T* p = at(row);
     if (p) *reinterpret_cast<u32x4_at2*>(p + chunk * X::VEC) = *reinterpret_cast<const u32x4*>(mine + row * X::ROWB + ((chunk ^ (row & (X::CPR - 1))) << 4));
+  }
+}
+
+// ... of one head, of which `have` exist, bfloat16: rows behind them are out of the descriptor's range
+template <int D> __device__ __forceinline__ void rows_out_head(const f32x16 (&acc)[D / 32], float factor, unsigned char* mine, int lane, bf16_t* to, uint32_t step, int have) {
+  typedef Mma<bf16_t, D> X;
+  const int l32 = lane & 31, hf = lane >> 5;
+  // chunk md * 4 + g4 of the lane's row, at (chunk ^ row) * 16
+  unsigned char* row = mine + l32 * X::ROWB + hf * 8;
+  const uint32_t turn = (uint32_t)(l32 & (X::CPR - 1)) << 4;
+#pragma unroll
+  for (int md = 0; md < D / 32; ++md)
+#pragma unroll
+    for (int g4 = 0; g4 < 4; ++g4)
+      *reinterpret_cast<u32x2*>(row + (turn ^ (uint32_t)((md * 4 + g4) << 4))) =
+          u32x2{f32_to_bf16_pair(acc[md][g4 * 4] * factor, acc[md][g4 * 4 + 1] * factor), f32_to_bf16_pair(acc[md][g4 * 4 + 2] * factor, acc[md][g4 * 4 + 3] * factor)};
+  constexpr int RPI = 64 / X::CPR;
+  const int r0 = lane / X::CPR, chunk = lane % X::CPR;
+  const auto rsrc = rows_rsrc(to, step, have, X::ROWB);
+  const int off = (int)((uint32_t)r0 * step) + chunk * 16;
+#pragma unroll
+  for (int i = 0; i < 32 / RPI; ++i)
+    __builtin_amdgcn_raw_buffer_store_b128(*reinterpret_cast<const u32x4*>(mine + (i * RPI + r0) * X::ROWB + ((chunk ^ ((i * RPI + r0) & (X::CPR - 1))) << 4)), rsrc, off,
+                                           (int)((uint32_t)(i * RPI) * step), 0);
+}
+// Row sums and outputs of a wavefront's 32 rows; l: the lane's half of the sum.
+template <typename T, int D, bool PART>
+__device__ __forceinline__ void fwd_out(const f32x16 (&acc)[D / 32], float m_run, float l_run, unsigned char* smem, T* O, float* lse, float* Opart, const CrossArgs& a, int bh, int part,
+                                        int wave, int lane, int row0) {
+  typedef Mma<T, D> X;
+  const int l32 = lane & 31, hf = lane >> 5, row = row0 + l32, b = bh / a.Hkv, hk = bh % a.Hkv;
+  const bool active = row < a.rows;
+  {
+    float p, q;
+    halves(l_run, p, q);
+    l_run = p + q;
+  }
+  const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+  const float stat = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * CROSS_LN2;
+  if constexpr (PART) {
+    if (!active) return;
+    const int64_t at = ((int64_t)part * a.B * a.Hkv + bh) * a.rows + row;
+    float* po = Opart + at * D;
+#pragma unroll
+    for (int md = 0; md < X::MD; ++md)
+#pragma unroll
+      for (int g4 = 0; g4 < 4; ++g4)
+        *reinterpret_cast<f32x4*>(po + md * 32 + g4 * 8 + hf * 4) = f32x4{acc[md][g4 * 4], acc[md][g4 * 4 + 1], acc[md][g4 * 4 + 2], acc[md][g4 * 4 + 3]} * inv;
+    if (hf == 0) lse[at] = stat;
+  } else {
+    if (lse && active && hf == 0) lse[((int64_t)b * a.Hq + hk * a.group) * a.N + row] = stat;
+    lds_ready();                              // everyone has read the last tile
+    rows_out<T, D>(acc, inv, smem + wave * 32 * X::ROWB, lane, [&](int r) __attribute__((always_inline)) -> T* {
+      if (row0 + r >= a.rows) return nullptr;
+      const CrossRow c = cross_row(a, row0 + r);
+      return O + b * a.o.b + (int64_t)(hk * a.group + c.g) * a.o.h + c.n * a.o.n;
+    });
   }
 }
 
@@ -301,6 +386,193 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void cross_fwd_kernel(con
       X::cols(acc, tile + TILEB + u * 32 * X::ROWB, cbase, X::weights(s[u]));
     }
   }
+  fwd_out<T, D, PART>(acc, m_run, l_run, smem, O, lse, Opart, a, bh, part, wave, lane, row0);
+}
+
+// bfloat16: the same, with the order of a tile fixed by hand.  A step makes the scores of tile t + 1 and the second product of tile t, and every MFMA is
+// followed by a slice of the vector work (exponentials of tile t, maximum of tile t + 1), about one weight a lane per MFMA, so that
+// one wavefront keeps both pipes busy; K is loaded a tile further ahead than V.
+template <int D, int NW, bool PART>
+__global__ __launch_bounds__(NW * 64, D == 64 ? 3 : 2) void cross_fwd_bf16_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V,
+                                                                     bf16_t* __restrict__ O, float* __restrict__ lse, float* __restrict__ Opart, CrossArgs a) {
+  typedef Mma<bf16_t, D> X;
+  constexpr int BN = 64, TILEB = BN * X::ROWB, OFF_V = 2 * TILEB, NA = 2 * X::KS, NB = 4 * X::MD, NPAIR = 16, NPA = 10, BSTRIDE = NB / 8, PF = 2;
+  static_assert((NPAIR - NPA - 1) * BSTRIDE < X::MD * 3 && 1 * BSTRIDE < X::MD * 2, "late weights are ready before the products that take them");
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * TILEB];   // K, K, V, V
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
+  const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int bh = blockIdx.y, b = bh / a.Hkv, hk = bh - b * a.Hkv, part = blockIdx.z;
+  const int len = seen_states(a, b);
+  const int t0 = part * a.tiles_per_part, tiles = (len + BN - 1) / BN, n = (t0 + a.tiles_per_part < tiles ? t0 + a.tiles_per_part : tiles) - t0;
+  const uint32_t lds = lds_address(smem);
+  TileStream<bf16_t, D, BN, NW> ks(K + b * a.k.b + hk * a.k.h + (int64_t)t0 * BN * a.k.n, (uint32_t)(a.k.n * 2), a.M - t0 * BN, wave, lane);
+  TileStream<bf16_t, D, BN, NW> vs(V + b * a.v.b + hk * a.v.h + (int64_t)t0 * BN * a.v.n, (uint32_t)(a.v.n * 2), a.M - t0 * BN, wave, lane);
+  auto byte_of = [&](int i) __attribute__((always_inline)) { return a.mask && i < n ? mask_byte(a, b, (t0 + i) * BN, len, lane) : 1; };
+  auto seen_of = [&](int byte, int i) __attribute__((always_inline)) -> uint64_t {
+    if (a.mask) return seen_bits(byte, (t0 + i) * BN, len, BN, lane);
+    const int have = len - (t0 + i) * BN;
+    return have >= 64 ? ~0ull : (1ull << have) - 1ull;
+  };
+  if (n > 0) ks.next(lds, wave);
+  int byte = byte_of(0), byte_next = byte_of(1);
+
+  // the wavefront's rows: of one head, or (flat) the next 32 of the key head's rows
+  const int head_blocks = a.flat ? 0x7fffffff : (a.N + NW * 32 - 1) / (NW * 32);
+  const int g = a.group == 1 || a.flat ? 0 : (int)blockIdx.x / head_blocks;
+  const int n0 = ((int)blockIdx.x - (a.flat ? 0 : g * head_blocks)) * (NW * 32) + wave * 32, row = n0 + l32;   // flat: rows of the key head
+  const int have = (a.flat ? a.rows : a.N) - n0;
+  typename X::Frag qf[X::KS];
+  if (a.flat) {
+    const CrossRow r = cross_row(a, row);
+    row_frags<bf16_t, D>(qf, Q + b * a.q.b + (int64_t)(hk * a.group + r.g) * a.q.h + r.n * a.q.n, hf, l32 < have);
+  } else {
+    const uint32_t step = (uint32_t)(a.q.n * 2);
+    const auto rsrc = rows_rsrc(Q + b * a.q.b + (int64_t)(hk * a.group + g) * a.q.h + (int64_t)n0 * a.q.n, step, have, X::ROWB);
+#pragma unroll
+    for (int k = 0; k < X::KS; ++k)
+      qf[k] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)((uint32_t)l32 * step) + hf * 16 + k * 32, 0, 0));
+  }
+  f32x16 acc[X::MD];
+#pragma unroll
+  for (int md = 0; md < X::MD; ++md)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[md][v] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f, shift = 0.f;
+  if (n > 0) {
+    vs.next(lds + OFF_V, wave);
+    if (n > 1) ks.next(lds + TILEB, wave);
+    const uint32_t rbase = rows_base<bf16_t, D>(lane), cbase = X::cols_base(lane);
+    uint64_t seen = seen_of(byte, 0), seen_next = 0;
+    auto advance = [&](float top) __attribute__((always_inline)) {
+      float p, q;
+      halves(top * a.scale_log2, p, q);
+      top = fmaxf(p, q);
+      const bool up = top - m_run > CROSS_LAZY;
+      if (__any(up)) {                        // (a row's own maximum decides: its bits do not depend on the rows beside it)
+        const float alpha = up ? __builtin_amdgcn_exp2f(m_run - top) : 1.f;
+        l_run *= alpha;
+#pragma unroll
+        for (int md = 0; md < X::MD; ++md)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) acc[md][v] *= alpha;
+        m_run = up ? top : m_run;
+      }
+      shift = m_run == -INFINITY ? 0.f : -m_run;
+    };
+    auto read_k = [&](int j, int buf) __attribute__((always_inline)) {       // product j: half j % 2 of the keys, k-step j / 2
+      return *reinterpret_cast<const bf16x8*>(smem + buf * TILEB + (j % 2) * 32 * X::ROWB + (rbase ^ (uint32_t)((j / 2) << 5)));
+    };
+    // weights 2q, 2q + 1 of the lane: registers of half q / 8
+    auto exp_pair = [&](const f32x16 (&s)[2], uint32_t (&w)[NPAIR], int q) __attribute__((always_inline)) {
+      const int u = q >> 3, v = 2 * (q & 7);
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(s[u][v], a.scale_log2, shift));
+      const float p1 = __builtin_amdgcn_exp2f(fmaf(s[u][v + 1], a.scale_log2, shift));
+      l_run += p0;
+      l_run += p1;
+      uint32_t bits = f32_to_bf16_pair(p0, p1);
+      asm volatile("" : "+v"(bits), "+v"(l_run));     // made here, not where it is used
+      w[q] = bits;
+    };
+    const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+
+    auto step = [&](auto parity, auto more_tag, f32x16 (&sc)[2], f32x16 (&sn)[2], int i) __attribute__((always_inline)) {
+      constexpr int PAR = decltype(parity)::value;
+      constexpr bool MORE = decltype(more_tag)::value;
+      tile_arrived();                         // K(i + 1), V(i)
+      if (MORE) {
+        seen_next = seen_of(byte_next, i + 1);
+        byte_next = byte_of(i + 2);
+        if (i + 2 < n) ks.next(lds + PAR * TILEB, wave);
+        vs.next(lds + OFF_V + (PAR ^ 1) * TILEB, wave);
+      }
+      unsigned char* vt = smem + OFF_V + PAR * TILEB;
+      if (seen != ~0ull) {
+        blank<bf16_t, D, NW * 64>(vt, BN, seen, tid);
+        lds_ready();
+      }
+      uint32_t w[NPAIR];
+      bf16x8 fr[4];
+      __builtin_amdgcn_sched_barrier(0);
+      if (MORE) {
+#pragma unroll
+        for (int j = 0; j < PF; ++j) fr[j] = read_k(j, PAR ^ 1);
+      }
+#pragma unroll
+      for (int j = 0; j < NA; ++j) {
+        if (MORE) {
+          if (j + PF < NA) fr[(j + PF) & 3] = read_k(j + PF, PAR ^ 1);
+          sn[j % 2] = X::mul(fr[j & 3], qf[j / 2], j < 2 ? zero : sn[j % 2]);
+        }
+#pragma unroll
+        for (int q = j * NPA / NA; q < (j + 1) * NPA / NA; ++q) exp_pair(sc, w, q);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (MORE && seen_next != ~0ull) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) hide(sn[u], (uint32_t)(seen_next >> (32 * u)), hf);
+      }
+      cs16x4 lo[4], hi[4];
+      auto read_v = [&](int j) __attribute__((always_inline)) {              // product j: channels j % MD, 16 keys j / MD
+        const uint32_t x = cbase ^ (uint32_t)((j % X::MD) << 6);
+        lo[j & 3] = X::read_t(vt + (j / X::MD) * 16 * X::ROWB + x);
+        hi[j & 3] = X::read_t(vt + ((j / X::MD) * 16 + 8) * X::ROWB + (x ^ 32u));
+      };
+      float top = -INFINITY;
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < PF; ++j) read_v(j);
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        if (j + PF < NB) read_v(j + PF);
+        const int md = j % X::MD, f = j / X::MD;
+        const bf16x8 pf = __builtin_bit_cast(bf16x8, (u32x4{w[4 * f], w[4 * f + 1], w[4 * f + 2], w[4 * f + 3]}));
+        acc[md] = X::mul(__builtin_bit_cast(bf16x8, (cs16x8)__builtin_shufflevector(lo[j & 3], hi[j & 3], 0, 1, 2, 3, 4, 5, 6, 7)), pf, acc[md]);
+        if (j % BSTRIDE == 0 && NPA + j / BSTRIDE < NPAIR) exp_pair(sc, w, NPA + j / BSTRIDE);
+        if (MORE) {
+#pragma unroll
+          for (int e = j * NPAIR / NB; e < (j + 1) * NPAIR / NB; ++e) top = fmaxf(top, fmaxf(sn[e >> 3][2 * (e & 7)], sn[e >> 3][2 * (e & 7) + 1]));
+          asm volatile("" ::"v"(top));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (MORE) {
+        advance(top);
+        seen = seen_next;
+      }
+    };
+
+    f32x16 sa[2], sb[2];
+    tile_arrived();                           // K(0) (and what was requested with it)
+#pragma unroll
+    for (int j = 0; j < NA; ++j) sa[j % 2] = X::mul(read_k(j, 0), qf[j / 2], j < 2 ? zero : sa[j % 2]);
+    if (seen != ~0ull) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) hide(sa[u], (uint32_t)(seen >> (32 * u)), hf);
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) top = fmaxf(top, sa[u][v]);
+    advance(top);
+    const std::integral_constant<int, 0> even;
+    const std::integral_constant<int, 1> odd;
+    const std::integral_constant<bool, true> more;
+    const std::integral_constant<bool, false> last;
+    int i = 0;
+    for (; i + 2 < n; i += 2) {
+      step(even, more, sa, sb, i);
+      step(odd, more, sb, sa, i + 1);
+    }
+    if (i + 1 < n) {
+      step(even, more, sa, sb, i);
+      step(odd, last, sb, sa, i + 1);
+    } else {
+      step(even, last, sa, sb, i);
+    }
+  }
+
+  // ---- the rows' sums and outputs
   {
     float p, q;
     halves(l_run, p, q);
@@ -309,23 +581,27 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void cross_fwd_kernel(con
   const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
   const float stat = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * CROSS_LN2;
   if constexpr (PART) {
-    if (!active) return;
-    const int64_t at = ((int64_t)part * a.B * a.Hkv + bh) * a.rows + row;
+    if (l32 >= have) return;
+    const int64_t at = ((int64_t)part * a.B * a.Hkv + bh) * a.rows + (int64_t)g * a.N + row;
     float* po = Opart + at * D;
+    if (hf == 0) lse[at] = stat;
 #pragma unroll
     for (int md = 0; md < X::MD; ++md)
 #pragma unroll
       for (int g4 = 0; g4 < 4; ++g4)
         *reinterpret_cast<f32x4*>(po + md * 32 + g4 * 8 + hf * 4) = f32x4{acc[md][g4 * 4], acc[md][g4 * 4 + 1], acc[md][g4 * 4 + 2], acc[md][g4 * 4 + 3]} * inv;
-    if (hf == 0) lse[at] = stat;
   } else {
-    if (lse && active && hf == 0) lse[((int64_t)b * a.Hq + hk * a.group) * a.N + row] = stat;
+    if (lse && hf == 0 && l32 < have) lse[((int64_t)b * a.Hq + hk * a.group + g) * a.N + row] = stat;
     lds_ready();                              // everyone has read the last tile
-    rows_out<T, D>(acc, inv, smem + wave * 32 * X::ROWB, lane, [&](int r) __attribute__((always_inline)) -> T* {
-      if (row0 + r >= a.rows) return nullptr;
-      const CrossRow c = cross_row(a, row0 + r);
-      return O + b * a.o.b + (int64_t)(hk * a.group + c.g) * a.o.h + c.n * a.o.n;
-    });
+    if (a.flat) {
+      rows_out<bf16_t, D>(acc, inv, smem + wave * 32 * X::ROWB, lane, [&](int r) __attribute__((always_inline)) -> bf16_t* {
+        if (r >= have) return nullptr;
+        const CrossRow c = cross_row(a, n0 + r);
+        return O + b * a.o.b + (int64_t)(hk * a.group + c.g) * a.o.h + c.n * a.o.n;
+      });
+    } else {
+      rows_out_head<D>(acc, inv, smem + wave * 32 * X::ROWB, lane, O + b * a.o.b + (int64_t)(hk * a.group + g) * a.o.h + (int64_t)n0 * a.o.n, (uint32_t)(a.o.n * 2), have);
+    }
   }
 }
 
@@ -593,6 +869,11 @@ static int cross_waves(const Plan& pl) {
   const int64_t rows = (int64_t)pl.group * pl.N;
   return rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
 }
+// Blocks of rows that hold rows of several heads: only where heads are so short that their last blocks, partly empty, would cost an eighth of the work.
+static bool cross_flat(const Plan& pl) {
+  const int64_t per = cross_waves(pl) * 32;
+  return pl.group > 1 && (pl.N + per - 1) / per * per * 8 > (int64_t)pl.N * 9;
+}
 static int cross_tile(const Plan& pl) { return pl.dtype == PSA_BF16 ? cross_keys<bf16_t>() : cross_keys<float>(); }
 // Workgroups that share the keys of a block of rows, where there are too few blocks to fill the chip: each at least four tiles.
 int cross_key_parts(const Plan& pl, int M) {
@@ -631,14 +912,21 @@ static void launch_cross_fwd_t(const Plan& pl, const CrossCall& c, const void* Q
   CrossArgs a = cross_args(pl, c);
   const int nw = cross_waves(pl);
   cross_share(a, cross_key_parts(pl, c.M), (c.M + cross_keys<T>() - 1) / cross_keys<T>());
-  const dim3 grid((unsigned)((a.rows + nw * 32 - 1) / (nw * 32)), (unsigned)(pl.B * pl.Hkv), (unsigned)a.parts);
+  a.flat = sizeof(T) == 4 || cross_flat(pl);
+  const dim3 grid((unsigned)(a.flat ? (a.rows + nw * 32 - 1) / (nw * 32) : pl.group * ((pl.N + nw * 32 - 1) / (nw * 32))), (unsigned)(pl.B * pl.Hkv), (unsigned)a.parts);
   const bool split = a.parts > 1;
   auto go = [&](auto kernel) {
     kernel<<<grid, nw * 64, 0, s>>>(static_cast<const T*>(Q), static_cast<const T*>(K), static_cast<const T*>(V), static_cast<T*>(O), split ? stats : lse, part, a);
   };
-  if (nw == 1) split ? go(cross_fwd_kernel<T, D, 1, true>) : go(cross_fwd_kernel<T, D, 1, false>);
-  else if (nw == 2) split ? go(cross_fwd_kernel<T, D, 2, true>) : go(cross_fwd_kernel<T, D, 2, false>);
-  else split ? go(cross_fwd_kernel<T, D, 4, true>) : go(cross_fwd_kernel<T, D, 4, false>);
+  if constexpr (sizeof(T) == 2) {
+    if (nw == 1) split ? go(cross_fwd_bf16_kernel<D, 1, true>) : go(cross_fwd_bf16_kernel<D, 1, false>);
+    else if (nw == 2) split ? go(cross_fwd_bf16_kernel<D, 2, true>) : go(cross_fwd_bf16_kernel<D, 2, false>);
+    else split ? go(cross_fwd_bf16_kernel<D, 4, true>) : go(cross_fwd_bf16_kernel<D, 4, false>);
+  } else {
+    if (nw == 1) split ? go(cross_fwd_kernel<T, D, 1, true>) : go(cross_fwd_kernel<T, D, 1, false>);
+    else if (nw == 2) split ? go(cross_fwd_kernel<T, D, 2, true>) : go(cross_fwd_kernel<T, D, 2, false>);
+    else split ? go(cross_fwd_kernel<T, D, 4, true>) : go(cross_fwd_kernel<T, D, 4, false>);
+  }
   if (!split) return;
   const int64_t total = (int64_t)pl.B * pl.Hq * pl.N, per = 256 / (D / 4);
   cross_join_kernel<T, D><<<(unsigned)((total + per - 1) / per), 256, 0, s>>>(part, stats, static_cast<T*>(O), lse, a);

@@ -52,9 +52,11 @@ def test_refusals_before_any_launch(lib):
     assert _fwd(lib, p, x(50, o=(0, 6400, 64))) == 1 and _fwd(lib, p, x(50, o=(25600, 0, 64))) == 1 and _fwd(lib, p, x(50, o=(25600, 64, 32))) == 1
     for name in ("dq", "dk", "dv"):
         assert _bwd(lib, p, x(50, **{name: (0, 6400, 64)})) == 1
-    # from one state to the next at most 32 MB
-    assert _fwd(lib, p, x(50, k=(2**40, 2**30, 2**24))) == 2 and _fwd(lib, p, x(50, v=(2**40, 2**30, 2**24))) == 2
-    assert _bwd(lib, p, x(50, q=(2**40, 2**30, 2**24))) == 2 and _bwd(lib, p, x(50, do=(2**40, 2**30, 2**24))) == 2
+    # from one token or state to the next at most 32 MB
+    for name in ("q", "k", "v", "o"):
+        assert _fwd(lib, p, x(50, **{name: (2**40, 2**33, 2**24)})) == 2
+    for name in ("q", "k", "v", "o", "do", "dq"):
+        assert _bwd(lib, p, x(50, **{name: (2**40, 2**33, 2**24)})) == 2
     wide = psa.make_params(1100, 60, 60, 4, 64, 64, 64, 4)
     assert _fwd(lib, wide, x(50)) == 2
     long_ = psa.make_params(1, 1024, 1, 4000000, 64, 64, 64, 4)
