@@ -418,7 +418,7 @@ static CrossLayout cross_layout(const Plan& pl, int M) {
   l.off_stats = kp > 1 ? align256(kp * rows * pl.d * e) : 0;
   l.fwd_bytes = kp > 1 ? l.off_stats + align256(kp * rows * e) : 0;
   size_t s = 0;
-  l.off_D = s;  s += align256(rows * e);
+  l.off_D = s;  s += align256(2 * rows * e);
   l.off_dq = s; s += kp > 1 ? align256(kp * rows * pl.d * e) : 0;
   l.off_dk = s; s += rp > 1 ? align256(rp * keys * pl.d * e) : 0;
   l.off_dv = s; s += rp > 1 ? align256(rp * keys * pl.d * e) : 0;
@@ -439,7 +439,7 @@ static int make_cross(const psa_params* p, const psa_cross* x, Plan* pl, CrossCa
   // offsets inside a tile of 64 rows are 32 bits wide, and so are the rows of a key head
   const int64_t most = ((int64_t)1 << 25) / pl->esize;
   if (c->k.n >= most || c->v.n >= most || c->q.n >= most || c->o.n >= most) return PSA_EUNSUPPORTED;
-  if (gradients && (c->go.n >= most || c->gq.n >= most)) return PSA_EUNSUPPORTED;
+  if (gradients && (c->go.n >= most || c->gq.n >= most || c->gk.n >= most || c->gv.n >= most)) return PSA_EUNSUPPORTED;
   if ((int64_t)B * Hkv > 65535 || (int64_t)pl->group * N > 0x7fffffff - 128 || M > 0x7fffffff - 128) return PSA_EUNSUPPORTED;
   return PSA_OK;
 }

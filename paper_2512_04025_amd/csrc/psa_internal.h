@@ -71,7 +71,7 @@ hipError_t launch_rotary(const Plan& pl, const psa_rotary_spec& r, int Hq, int H
                          const int32_t* perm, bool inverse, const void* Qin, const void* Kin, void* Qout, void* Kout, hipStream_t s);
 void rotary_spectrum_host(int d, int axes, const int32_t* pairs, double base, bool shared, psa_rotary_spec* r);
 // Cross attention to M states.  part, stats / dQpart / dKpart, dVpart: partial results in fp32 (cross_key_parts or cross_row_parts times the
-// result's elements; unused where that is 1); Dr: a float per query row.
+// result's elements; unused where that is 1); Dr: two floats per query row.
 struct CrossCall {
   int M;
   Strides q, k, v, o, gq, gk, gv, go;         // g: the gradients

@@ -55,7 +55,7 @@ def test_refusals_before_any_launch(lib):
     # from one token or state to the next at most 32 MB
     for name in ("q", "k", "v", "o"):
         assert _fwd(lib, p, x(50, **{name: (2**40, 2**33, 2**24)})) == 2
-    for name in ("q", "k", "v", "o", "do", "dq"):
+    for name in ("q", "k", "v", "o", "do", "dq", "dk", "dv"):
         assert _bwd(lib, p, x(50, **{name: (2**40, 2**33, 2**24)})) == 2
     wide = psa.make_params(1100, 60, 60, 4, 64, 64, 64, 4)
     assert _fwd(lib, wide, x(50)) == 2
