@@ -413,13 +413,13 @@ struct CrossLayout { size_t off_part, off_stats, fwd_bytes, off_D, off_dq, off_d
 static CrossLayout cross_layout(const Plan& pl, int M) {
   CrossLayout l;
   const size_t rows = (size_t)pl.B * pl.Hq * pl.N, keys = (size_t)pl.B * pl.Hkv * M, e = sizeof(float);
-  const size_t kp = cross_key_parts(pl, M), rp = cross_row_parts(pl, M);
+  const size_t kf = cross_key_parts(pl, M, false), kb = cross_key_parts(pl, M, true), rp = cross_row_parts(pl, M);
   l.off_part = 0;
-  l.off_stats = kp > 1 ? align256(kp * rows * pl.d * e) : 0;
-  l.fwd_bytes = kp > 1 ? l.off_stats + align256(kp * rows * e) : 0;
+  l.off_stats = kf > 1 ? align256(kf * rows * pl.d * e) : 0;
+  l.fwd_bytes = kf > 1 ? l.off_stats + align256(kf * rows * e) : 0;
   size_t s = 0;
   l.off_D = s;  s += align256(2 * rows * e);
-  l.off_dq = s; s += kp > 1 ? align256(kp * rows * pl.d * e) : 0;
+  l.off_dq = s; s += kb > 1 ? align256(kb * rows * pl.d * e) : 0;
   l.off_dk = s; s += rp > 1 ? align256(rp * keys * pl.d * e) : 0;
   l.off_dv = s; s += rp > 1 ? align256(rp * keys * pl.d * e) : 0;
   l.bwd_bytes = s;

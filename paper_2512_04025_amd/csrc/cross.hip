@@ -610,22 +610,41 @@ __global__ __launch_bounds__(NW * 64, D == 64 ? 3 : 2) void cross_fwd_bf16_kerne
   }
 }
 
-// Rows of a part each -> the row: O = sum w O_part / sum w, w = exp(lse_part - their maximum).
+// Rows of a part each -> the row: O = sum w O_part / sum w, w = exp(lse_part - their maximum).  Eight parts' loads at a time: the kernel is latency.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cross_join_kernel(const float* __restrict__ Opart, const float* __restrict__ stats, T* __restrict__ O, float* __restrict__ lse, CrossArgs a) {
-  constexpr int LANES = D / 4;
+  constexpr int LANES = D / 4, AHEAD = 8;
   const int64_t total = (int64_t)a.B * a.Hkv * a.rows, x = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
   if (x >= total) return;
   const int c = threadIdx.x % LANES;
-  float top = -INFINITY;
-  for (int s = 0; s < a.parts; ++s) top = fmaxf(top, stats[s * total + x]);
+  // One pass with the running maximum of a softmax, a batch at a time
+  float top = -INFINITY, weight = 0.f;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  float weight = 0.f;
-  for (int s = 0; s < a.parts; ++s) {
-    const float w = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((stats[s * total + x] - top) * CROSS_LOG2E);
-    const f32x4 o = *reinterpret_cast<const f32x4*>(Opart + (s * total + x) * D + c * 4);
-    weight += w;
-    sum += o * w;
+  for (int s0 = 0; s0 < a.parts; s0 += AHEAD) {
+    float l[AHEAD];
+    f32x4 o[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int s = s0 + u < a.parts ? s0 + u : a.parts - 1;
+      l[u] = stats[s * total + x];
+      o[u] = *reinterpret_cast<const f32x4*>(Opart + (s * total + x) * D + c * 4);
+    }
+    float most = top;
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) most = fmaxf(most, l[u]);
+    const float base = most == -INFINITY ? 0.f : most;      // (parts that see nothing have weight 0, one that is not a number spoils the row)
+    const float keep = __builtin_amdgcn_exp2f((top - base) * CROSS_LOG2E);
+    weight *= keep;
+    sum *= keep;
+    top = most;
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const float w = __builtin_amdgcn_exp2f((l[u] - base) * CROSS_LOG2E);
+      if (s0 + u < a.parts) {
+        weight += w;
+        sum += o[u] * w;
+      }
+    }
   }
   const float inv = weight == 0.f ? 0.f : 1.f / weight;
   const int bh = (int)(x / a.rows), row = (int)(x - (int64_t)bh * a.rows), b = bh / a.Hkv, hk = bh % a.Hkv;
@@ -1239,17 +1258,33 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cross_dkv_bf16_kernel(co
   }
 }
 
-// out[b, h, l, :] = factor * sum over the parts, in their order
-template <typename T, int D>
-__global__ __launch_bounds__(256) void cross_sum_kernel(const float* __restrict__ part, T* __restrict__ out, int H, int L, int64_t total, int parts, float factor, Strides to) {
-  constexpr int LANES = D / 4;
+// out[b, h, l, :] = factor * sum over the parts, in their order; two tensors of one shape in one launch (blockIdx.y)
+template <typename T> struct CrossSum {
+  const float* part[2];
+  T* out[2];
+  float factor[2];
+  Strides to[2];
+  int H, L, parts;
+  int64_t total;                              // rows
+};
+template <typename T, int D> __global__ __launch_bounds__(256) void cross_sum_kernel(CrossSum<T> p) {
+  constexpr int LANES = D / 4, AHEAD = 8;
   const int64_t x = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-  if (x >= total) return;
-  const int c = threadIdx.x % LANES;
+  if (x >= p.total) return;
+  const int c = threadIdx.x % LANES, which = blockIdx.y;
+  const float* part = p.part[which] + x * D + c * 4;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < parts; ++s) sum += *reinterpret_cast<const f32x4*>(part + (s * total + x) * D + c * 4);
-  const int64_t bh = x / L;
-  Four<T>::store(out + bh / H * to.b + bh % H * to.h + (x - bh * L) * to.n + c * 4, sum * factor);
+  for (int s0 = 0; s0 < p.parts; s0 += AHEAD) {
+    f32x4 v[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) v[u] = *reinterpret_cast<const f32x4*>(part + (s0 + u < p.parts ? s0 + u : p.parts - 1) * p.total * D);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (s0 + u < p.parts) sum += v[u];
+  }
+  const Strides to = p.to[which];
+  const int64_t bh = x / p.L;
+  Four<T>::store(p.out[which] + bh / p.H * to.b + bh % p.H * to.h + (x - bh * p.L) * to.n + c * 4, sum * p.factor[which]);
 }
 
 // ---- host
@@ -1259,28 +1294,54 @@ static int cross_waves(const Plan& pl) {
   const int64_t rows = (int64_t)pl.group * pl.N;
   return rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
 }
-// Blocks of rows that hold rows of several heads: only where heads are so short that their last blocks, partly empty, would cost an eighth of the work.
+// Blocks of rows that hold rows of several heads: float32; bfloat16, whose rows of one head are addressed as one range, only where heads are so short that their last blocks, partly empty, would cost an eighth of the work.
 static bool cross_flat(const Plan& pl) {
+  if (pl.dtype != PSA_BF16) return true;
   const int64_t per = cross_waves(pl) * 32;
   return pl.group > 1 && (pl.N + per - 1) / per * per * 8 > (int64_t)pl.N * 9;
 }
 static int cross_tile(const Plan& pl) { return pl.dtype == PSA_BF16 ? cross_keys<bf16_t>() : cross_keys<float>(); }
-// Workgroups that share the keys of a block of rows, where there are too few blocks to fill the chip: each at least four tiles.
-int cross_key_parts(const Plan& pl, int M) {
-  const int64_t rows = (int64_t)pl.group * pl.N, per = cross_waves(pl) * 32, blocks = (rows + per - 1) / per * pl.B * pl.Hkv;
-  const int tiles = (M + cross_tile(pl) - 1) / cross_tile(pl);
-  int64_t parts = 512 / blocks, most = tiles / 4;
-  parts = parts < most ? parts : most;
-  return parts < 1 ? 1 : (int)parts;
+
+// How many workgroups share the tiles of a block (the keys of a block of rows, the rows of a block of keys), each leaving a partial result that is read and added up by
+// another kernel.  The number that is expected to take least: with w workgroups on a compute unit a tile takes them w * busy, but no less than `lone`, a
+// workgroup costs `start` besides (as many as fit at one time: once), and the parts cost what they move and 5 us for the launch.
+struct CrossCost { double busy, lone, start; int fit; };                 // us
+static int cross_parts(int64_t blocks, int64_t tiles, const CrossCost& c, double part_bytes) {
+  int best = 1;
+  double least = 0.0;
+  for (int64_t p = 1; p <= 128 && p <= (tiles > 1 ? tiles : 1); ++p) {
+    const int64_t w = (blocks * p + 255) / 256, each = (tiles + p - 1) / p;
+    const double us = (double)each * (w * c.busy > c.lone ? w * c.busy : c.lone) + (double)((w + c.fit - 1) / c.fit) * c.start + (p > 1 ? 5.0 + (double)p * part_bytes / 1.75e6 : 0.0);
+    if (p == 1 || us < least) {
+      least = us;
+      best = (int)p;
+    }
+  }
+  return best;
 }
-// Workgroups that share the rows of a block of 128 keys: each at least eight tiles.
+// Measured: bfloat16, us of a tile of 64 with the chip full and for a workgroup alone; float32: the rate of its matrix instructions (0.98 us of 32 x 32 x 64 on a SIMD).
+int cross_key_parts(const Plan& pl, int M, bool gradient) {
+  const int nw = cross_waves(pl);
+  const int64_t per = nw * 32, blocks = (cross_flat(pl) ? ((int64_t)pl.group * pl.N + per - 1) / per : pl.group * ((pl.N + per - 1) / per)) * pl.B * pl.Hkv;
+  const int64_t tiles = ((int64_t)M + cross_tile(pl) - 1) / cross_tile(pl);
+  CrossCost c;
+  if (pl.dtype == PSA_BF16) {
+    if (pl.d == 128) c = gradient ? CrossCost{1.35, 2.0, 5.0, 2} : CrossCost{0.9, 1.3, 4.0, 2};
+    else c = gradient ? CrossCost{0.75, 1.4, 5.0, 2} : CrossCost{0.47, 1.0, 4.0, nw == 4 ? 3 : 5};
+    c.busy *= nw / 4.0;
+  } else {
+    const double us = (gradient ? 3 : 2) * (pl.d == 128 ? 1.96 : 0.98);
+    c = CrossCost{us * nw / 4.0, us, 4.0, pl.d == 128 ? (gradient ? 1 : 2) : (gradient ? 2 : 4)};
+  }
+  return cross_parts(blocks, tiles, c, 4.0 * pl.B * pl.Hq * (double)pl.N * pl.d);
+}
 int cross_row_parts(const Plan& pl, int M) {
-  const int64_t blocks = (int64_t)(M + 127) / 128 * pl.B * pl.Hkv;
+  const int64_t blocks = ((int64_t)M + 127) / 128 * pl.B * pl.Hkv, tiles = (int64_t)pl.group * ((pl.N + cross_tile(pl) - 1) / cross_tile(pl));
   if (blocks == 0) return 1;
-  const int64_t tiles = (int64_t)pl.group * ((pl.N + cross_tile(pl) - 1) / cross_tile(pl));
-  int64_t parts = 512 / blocks, most = tiles / 8;
-  parts = parts < most ? parts : most;
-  return parts < 1 ? 1 : (int)parts;
+  CrossCost c;
+  if (pl.dtype == PSA_BF16) c = pl.d == 128 ? CrossCost{1.5, 2.2, 5.0, 2} : CrossCost{0.8, 1.5, 5.0, 3};
+  else c = pl.d == 128 ? CrossCost{7.8, 7.8, 5.0, 1} : CrossCost{3.9, 3.9, 5.0, 2};
+  return cross_parts(blocks, tiles, c, 8.0 * pl.B * pl.Hkv * (double)M * pl.d);
 }
 
 static CrossArgs cross_args(const Plan& pl, const CrossCall& c) {
@@ -1301,8 +1362,8 @@ template <typename T, int D>
 static void launch_cross_fwd_t(const Plan& pl, const CrossCall& c, const void* Q, const void* K, const void* V, void* O, float* lse, float* part, float* stats, hipStream_t s) {
   CrossArgs a = cross_args(pl, c);
   const int nw = cross_waves(pl);
-  cross_share(a, cross_key_parts(pl, c.M), (c.M + cross_keys<T>() - 1) / cross_keys<T>());
-  a.flat = sizeof(T) == 4 || cross_flat(pl);
+  cross_share(a, cross_key_parts(pl, c.M, false), (c.M + cross_keys<T>() - 1) / cross_keys<T>());
+  a.flat = cross_flat(pl);
   const dim3 grid((unsigned)(a.flat ? (a.rows + nw * 32 - 1) / (nw * 32) : pl.group * ((pl.N + nw * 32 - 1) / (nw * 32))), (unsigned)(pl.B * pl.Hkv), (unsigned)a.parts);
   const bool split = a.parts > 1;
   auto go = [&](auto kernel) {
@@ -1334,8 +1395,8 @@ static void launch_cross_bwd_t(const Plan& pl, const CrossCall& c, const void* Q
   CrossArgs a = cross_args(pl, c);
   const T *q = static_cast<const T*>(Q), *k = static_cast<const T*>(K), *v = static_cast<const T*>(V), *o = static_cast<const T*>(O), *g = static_cast<const T*>(dO);
   const int nw = cross_waves(pl), per = 256 / (D / 4);
-  cross_share(a, cross_key_parts(pl, c.M), (c.M + cross_keys<T>() - 1) / cross_keys<T>());
-  a.flat = sizeof(T) == 4 || cross_flat(pl);
+  cross_share(a, cross_key_parts(pl, c.M, true), (c.M + cross_keys<T>() - 1) / cross_keys<T>());
+  a.flat = cross_flat(pl);
   {
     const dim3 grid((unsigned)(a.flat ? (a.rows + nw * 32 - 1) / (nw * 32) : pl.group * ((pl.N + nw * 32 - 1) / (nw * 32))), (unsigned)(pl.B * pl.Hkv), (unsigned)a.parts);
     const bool split = a.parts > 1;
@@ -1350,7 +1411,9 @@ static void launch_cross_bwd_t(const Plan& pl, const CrossCall& c, const void* Q
       else split ? go(cross_dq_kernel<T, D, 4, true>) : go(cross_dq_kernel<T, D, 4, false>);
     }
     const int64_t total = (int64_t)pl.B * pl.Hq * pl.N;
-    if (split) cross_sum_kernel<T, D><<<(unsigned)((total + per - 1) / per), 256, 0, s>>>(dQpart, static_cast<T*>(dQ), pl.Hq, pl.N, total, a.parts, pl.scale, c.gq);
+    if (split)
+      cross_sum_kernel<T, D><<<dim3((unsigned)((total + per - 1) / per), 1), 256, 0, s>>>(
+          CrossSum<T>{{dQpart, nullptr}, {static_cast<T*>(dQ), nullptr}, {pl.scale, 0.f}, {c.gq, c.gq}, pl.Hq, pl.N, a.parts, total});
   }
   if (c.M == 0) return;
   cross_share(a, cross_row_parts(pl, c.M), pl.group * a.chunks);
@@ -1366,9 +1429,8 @@ static void launch_cross_bwd_t(const Plan& pl, const CrossCall& c, const void* Q
   if (a.parts > 1) {
     gradients(std::true_type{});
     const int64_t total = (int64_t)pl.B * pl.Hkv * c.M;
-    const unsigned n = (unsigned)((total + per - 1) / per);
-    cross_sum_kernel<T, D><<<n, 256, 0, s>>>(dKpart, static_cast<T*>(dK), pl.Hkv, c.M, total, a.parts, pl.scale, c.gk);
-    cross_sum_kernel<T, D><<<n, 256, 0, s>>>(dVpart, static_cast<T*>(dV), pl.Hkv, c.M, total, a.parts, 1.f, c.gv);
+    cross_sum_kernel<T, D><<<dim3((unsigned)((total + per - 1) / per), 2), 256, 0, s>>>(
+        CrossSum<T>{{dKpart, dVpart}, {static_cast<T*>(dK), static_cast<T*>(dV)}, {pl.scale, 1.f}, {c.gk, c.gv}, pl.Hkv, c.M, a.parts, total});
   } else {
     gradients(std::false_type{});
   }

@@ -78,7 +78,7 @@ struct CrossCall {
   const int32_t* kv_len;
   const uint8_t* key_mask;
 };
-int cross_key_parts(const Plan& pl, int M);
+int cross_key_parts(const Plan& pl, int M, bool gradient);
 int cross_row_parts(const Plan& pl, int M);
 hipError_t launch_cross_fwd(const Plan& pl, const CrossCall& c, const void* Q, const void* K, const void* V, void* O, float* lse, float* part, float* stats, hipStream_t s);
 hipError_t launch_cross_bwd(const Plan& pl, const CrossCall& c, const void* Q, const void* K, const void* V, const void* O, const float* lse, const void* dO, void* dQ, void* dK,

@@ -230,6 +230,21 @@ def test_infinite_and_nan_inputs_stay_in_their_rows(dtype):
     assert torch.equal(a.O[same], clean[same])
 
 
+def test_a_row_that_is_not_finite_spoils_its_own_parts():
+    """The same where workgroups share the states."""
+    import torch
+    for dtype in ("bf16", "f32"):
+        a = Problem(dtype, 64, 1, 1, 1, 40, 5000)
+        assert psa.psa_query_cross_sizes(a.p, 5000)[0] > 0
+        a.forward()
+        clean = a.O.clone()
+        a.Q[0, 0, 7, 5] = float("nan")
+        a.forward()
+        assert torch.all(torch.isnan(a.O[0, 0, 7])) and torch.isnan(a.lse[0, 0, 7])
+        ok = [i for i in range(40) if i != 7]
+        assert torch.equal(a.O[:, :, ok], clean[:, :, ok])
+
+
 @pytest.mark.parametrize("dtype,N,M", [("bf16", 300, 200), ("bf16", 4, 4000), ("f32", 130, 90)])
 def test_bits_repeat_on_other_streams_and_in_graphs(dtype, N, M):
     import torch
