@@ -213,10 +213,8 @@ def _rows(x, shape, dtype, strides, device: int):
     """Device pointer of a [B, H, L, d] tensor that the kernels address by `strides` ((0, 0, 0): contiguous)."""
     if x is None:
         return None
-    if x.shape != shape or x.dtype != dtype:
-        raise ValueError(f"expected a {dtype} tensor of shape {tuple(shape)}, got {x.dtype} {tuple(x.shape)}")
-    if x.get_device() != device:
-        raise ValueError("libpsa takes tensors of the current device")
+    if x.shape != shape or x.dtype is not dtype or x.get_device() != device:
+        raise ValueError(f"expected a {dtype} tensor of shape {tuple(shape)} on the current device, got {x.dtype} {tuple(x.shape)} on {x.device}")
     if strides == _CONTIGUOUS:
         if not x.is_contiguous():
             raise ValueError("the tensor is not contiguous: give its strides to the spec")
@@ -236,15 +234,23 @@ def _table(x, shapes, dtype, device: int, what):
     return x.data_ptr()
 
 
+_torch = None
+
+
 def _here(p: PsaParams, stream):
     """The library, torch, the current device, its stream to work on, p's element type."""
-    import torch
-    dev = torch.cuda.current_device()
+    global _torch
+    torch = _torch
+    if torch is None:
+        import torch
+        torch.cuda.init()
+        _torch = torch
+    dev = torch._C._cuda_getDevice()
     if stream is None:
         stream = torch._C._cuda_getCurrentRawStream(dev)
     else:
         stream = getattr(stream, "cuda_stream", stream)
-    return _lib or load_library(), torch, dev, stream or None, torch.bfloat16 if p.dtype == PSA_BF16 else torch.float32
+    return _lib or load_library(), torch, dev, stream or None, torch.float32 if p.dtype else torch.bfloat16
 
 
 def make_rotary(d: int, pairs: Sequence[int], base: float = 10000.0, shared: bool = False, pairing: int = PSA_ROTARY_ADJACENT,

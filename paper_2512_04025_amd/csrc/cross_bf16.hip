@@ -440,7 +440,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cross_dkv_bf16_kernel(co
   const int key0 = (int)(blockIdx.x * (NW * 32) + wave * 32), key = key0 + l32;
   const int len = __builtin_amdgcn_readfirstlane(seen_states(a, b));
   const bool seen = key < len && (!a.mask || a.mask[(int64_t)b * a.M + key] != 0);
-  const bool any = __syncthreads_or(seen);
+  const bool any = __syncthreads_or(seen), mine = __any(seen);       // a wavefront none of whose keys is seen loads for the others
   const int all = any ? a.group * a.chunks : 0;
   const int t0 = part * a.tiles_per_part, t1 = t0 + a.tiles_per_part < all ? t0 + a.tiles_per_part : all;
   const uint32_t lds = lds_address(smem);
@@ -508,7 +508,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cross_dkv_bf16_kernel(co
       }
 #pragma unroll 1
       for (int u = 0; u < 2; ++u) {
-        if (u * 32 >= have) break;
+        if (u * 32 >= have || !mine) break;
         const unsigned char* qt = tile + u * 32 * X::ROWB;
         const float* sl = stat + u * 32 + (lane_again() >> 5) * 4;
         Fragments<D, D == 128> fr;

@@ -295,7 +295,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void cross_dkv_f32_kernel(con
   const int key0 = (int)(blockIdx.x * (NW * 32) + wave * 32), key = key0 + l32;
   const int len = __builtin_amdgcn_readfirstlane(seen_states(a, b));
   const bool seen = key < len && (!a.mask || a.mask[(int64_t)b * a.M + key] != 0);
-  const bool any = __syncthreads_or(seen);
+  const bool any = __syncthreads_or(seen), mine = __any(seen);       // a wavefront none of whose keys is seen loads for the others
   const int all = any ? a.group * a.chunks : 0;
   const int t0 = part * a.tiles_per_part, t1 = t0 + a.tiles_per_part < all ? t0 + a.tiles_per_part : all;
   const uint32_t lds = lds_address(smem), qstep = (uint32_t)(a.q.n * 4), gstep = (uint32_t)(a.go.n * 4);
@@ -335,6 +335,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void cross_dkv_f32_kernel(con
       }
       lds_ready();
     }
+    if (!mine) continue;
     f32x16 two[2];
     rows<D, 2>(two, {tile, tile + TILEB}, lane, {&kr, &vr});
     f32x16 &s = two[0], &g = two[1];
