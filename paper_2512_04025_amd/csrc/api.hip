@@ -426,6 +426,23 @@ static CrossLayout cross_layout(const Plan& pl, int M) {
   return l;
 }
 
+// Query heads of a key head whose rows follow each other in equal steps (one token each, or contiguous heads) are one head of group * N tokens: fewer blocks of rows that are
+// partly empty, nothing to tell heads apart.
+static void merge_heads(Plan* pl, CrossCall* c, bool gradients) {
+  Strides* const row_tensors[4] = {&c->q, &c->o, &c->go, &c->gq};
+  const int64_t most = ((int64_t)1 << 25) / pl->esize;
+  if (pl->group == 1 || (int64_t)pl->group * pl->N > 0x7fffffff - 128) return;
+  for (int i = 0; i < (gradients ? 4 : 2); ++i)
+    if (pl->N == 1 ? row_tensors[i]->h >= most : row_tensors[i]->h != (int64_t)pl->N * row_tensors[i]->n) return;
+  for (int i = 0; i < (gradients ? 4 : 2); ++i) {
+    if (pl->N == 1) row_tensors[i]->n = row_tensors[i]->h;
+    row_tensors[i]->h *= pl->group;
+  }
+  pl->N *= pl->group;
+  pl->Hq = pl->Hkv;
+  pl->group = 1;
+}
+
 static int make_cross(const psa_params* p, const psa_cross* x, Plan* pl, CrossCall* c, bool gradients) {
   const int rc = make_plan(p, pl);
   if (rc != PSA_OK) return rc;
@@ -449,9 +466,14 @@ int psa_query_cross_sizes(const psa_params* p, const psa_cross* x, size_t* fwd_s
   CrossCall c;
   const int rc = make_cross(p, x, &pl, &c, true);
   if (rc != PSA_OK) return rc;
-  const CrossLayout l = cross_layout(pl, c.M);
-  if (fwd_scratch) *fwd_scratch = l.fwd_bytes;
-  if (bwd_scratch) *bwd_scratch = l.bwd_bytes;
+  // the same for all strides: with and without merged heads
+  CrossLayout l = cross_layout(pl, c.M);
+  pl.N *= pl.group;
+  pl.Hq = pl.Hkv;
+  pl.group = 1;
+  const CrossLayout m = cross_layout(pl, c.M);
+  if (fwd_scratch) *fwd_scratch = l.fwd_bytes > m.fwd_bytes ? l.fwd_bytes : m.fwd_bytes;
+  if (bwd_scratch) *bwd_scratch = l.bwd_bytes > m.bwd_bytes ? l.bwd_bytes : m.bwd_bytes;
   return PSA_OK;
 }
 
@@ -462,6 +484,7 @@ int psa_cross_attention_fwd(const psa_params* p, const psa_cross* x, const void*
   const int rc = make_cross(p, x, &pl, &c, false);
   if (rc != PSA_OK) return rc;
   if (!Q || !O || (c.M > 0 && (!K || !V))) return PSA_EINVAL;
+  merge_heads(&pl, &c, false);
   const CrossLayout l = cross_layout(pl, c.M);
   if (l.fwd_bytes && (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255))) return PSA_EINVAL;
   c.kv_len = kv_len;
@@ -479,6 +502,7 @@ int psa_cross_attention_bwd(const psa_params* p, const psa_cross* x, const void*
   if (rc != PSA_OK) return rc;
   if (!Q || !O || !lse || !dO || !dQ || !scratch || (c.M > 0 && (!K || !V || !dK || !dV))) return PSA_EINVAL;
   if (reinterpret_cast<uintptr_t>(scratch) & 255) return PSA_EINVAL;
+  merge_heads(&pl, &c, true);
   const CrossLayout l = cross_layout(pl, c.M);
   c.kv_len = kv_len;
   c.key_mask = key_mask;

@@ -56,33 +56,35 @@ __global__ __launch_bounds__(256) void cross_join_kernel(const float* __restrict
   if (lse && c == 0) lse[((int64_t)b * a.Hq + hk * a.group) * a.N + row] = weight == 0.f ? -INFINITY : top + log2f(weight) * CROSS_LN2;
 }
 
-// out[b, h, l, :] = factor * sum over the parts, in their order; two tensors of one shape in one launch (blockIdx.y)
+// out[b, h, l, :] = factor * sum over the parts, in their order; up to three tensors in one launch (blockIdx.y)
 template <typename T> struct CrossSum {
-  const float* part[2];
-  T* out[2];
-  float factor[2];
-  Strides to[2];
-  int H, L, parts;
-  int64_t total;                              // rows
+  struct One {
+    const float* part;
+    T* out;
+    int64_t rows;
+    Strides to;
+    int H, L, parts;
+    float factor;
+  } of[3];
 };
 template <typename T, int D> __global__ __launch_bounds__(256) void cross_sum_kernel(CrossSum<T> p) {
   constexpr int LANES = D / 4, AHEAD = 8;
+  const auto& o = p.of[blockIdx.y];
   const int64_t x = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-  if (x >= p.total) return;
-  const int c = threadIdx.x % LANES, which = blockIdx.y;
-  const float* part = p.part[which] + x * D + c * 4;
+  if (x >= o.rows) return;
+  const int c = threadIdx.x % LANES;
+  const float* part = o.part + x * D + c * 4;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < p.parts; s0 += AHEAD) {
+  for (int s0 = 0; s0 < o.parts; s0 += AHEAD) {
     f32x4 v[AHEAD];
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) v[u] = *reinterpret_cast<const f32x4*>(part + (s0 + u < p.parts ? s0 + u : p.parts - 1) * p.total * D);
+    for (int u = 0; u < AHEAD; ++u) v[u] = *reinterpret_cast<const f32x4*>(part + (s0 + u < o.parts ? s0 + u : o.parts - 1) * o.rows * D);
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
-      if (s0 + u < p.parts) sum += v[u];
+      if (s0 + u < o.parts) sum += v[u];
   }
-  const Strides to = p.to[which];
-  const int64_t bh = x / p.L;
-  Four<T>::store(p.out[which] + bh / p.H * to.b + bh % p.H * to.h + (x - bh * p.L) * to.n + c * 4, sum * p.factor[which]);
+  const int64_t bh = x / o.L;
+  Four<T>::store(o.out + bh / o.H * o.to.b + bh % o.H * o.to.h + (x - bh * o.L) * o.to.n + c * 4, sum * o.factor);
 }
 
 // ---- host
@@ -190,18 +192,30 @@ static void launch_cross_bwd_t(const Plan& pl, const CrossCall& c, const void* Q
   const T *q = static_cast<const T*>(Q), *k = static_cast<const T*>(K), *v = static_cast<const T*>(V), *o = static_cast<const T*>(O), *g = static_cast<const T*>(dO);
   T *gq = static_cast<T*>(dQ), *gk = static_cast<T*>(dK), *gv = static_cast<T*>(dV);
   const int nw = cross_waves(pl);
-  auto sum = [&](const CrossSum<T>& x, int tensors) {
-    const dim3 grid(cross_rows_of_256(x.total, pl.d), (unsigned)tensors);
-    if (pl.d == 128) cross_sum_kernel<T, 128><<<grid, 256, 0, s>>>(x);
-    else cross_sum_kernel<T, 64><<<grid, 256, 0, s>>>(x);
+  CrossSum<T> sums;
+  int tensors = 0;
+  int64_t most = 0;
+  auto add = [&](const float* part, T* out, int H, int L, const Strides& to, float factor) {
+    const int64_t rows = (int64_t)pl.B * H * L;
+    sums.of[tensors++] = {part, out, rows, to, H, L, a.parts, factor};
+    if (rows > most) most = rows;
   };
   cross_share(a, cross_key_parts(pl, c.M, true), (c.M + cross_keys<T>() - 1) / cross_keys<T>());
   cross_dq(a, pl.d, cross_row_grid(pl, a, nw), nw, a.parts > 1, q, k, v, o, lse, g, Dr, gq, dQpart, s);
-  if (a.parts > 1) sum({{dQpart, nullptr}, {gq, nullptr}, {pl.scale, 0.f}, {c.gq, c.gq}, pl.Hq, pl.N, a.parts, (int64_t)pl.B * pl.Hq * pl.N}, 1);
-  if (c.M == 0) return;
-  cross_share(a, cross_row_parts(pl, c.M), pl.group * a.chunks);
-  cross_dkv(a, pl.d, dim3((unsigned)((c.M + 127) / 128), (unsigned)(pl.B * pl.Hkv), (unsigned)a.parts), a.parts > 1, q, k, v, Dr, g, gk, gv, dKpart, dVpart, s);
-  if (a.parts > 1) sum({{dKpart, dVpart}, {gk, gv}, {pl.scale, 1.f}, {c.gk, c.gv}, pl.Hkv, c.M, a.parts, (int64_t)pl.B * pl.Hkv * c.M}, 2);
+  if (a.parts > 1) add(dQpart, gq, pl.Hq, pl.N, c.gq, pl.scale);
+  if (c.M > 0) {
+    cross_share(a, cross_row_parts(pl, c.M), pl.group * a.chunks);
+    cross_dkv(a, pl.d, dim3((unsigned)((c.M + 127) / 128), (unsigned)(pl.B * pl.Hkv), (unsigned)a.parts), a.parts > 1, q, k, v, Dr, g, gk, gv, dKpart, dVpart, s);
+    if (a.parts > 1) {
+      add(dKpart, gk, pl.Hkv, c.M, c.gk, pl.scale);
+      add(dVpart, gv, pl.Hkv, c.M, c.gv, 1.f);
+    }
+  }
+  if (tensors == 0) return;
+  for (int i = tensors; i < 3; ++i) sums.of[i] = sums.of[0];
+  const dim3 grid(cross_rows_of_256(most, pl.d), (unsigned)tensors);
+  if (pl.d == 128) cross_sum_kernel<T, 128><<<grid, 256, 0, s>>>(sums);
+  else cross_sum_kernel<T, 64><<<grid, 256, 0, s>>>(sums);
 }
 
 hipError_t launch_cross_bwd(const Plan& pl, const CrossCall& c, const void* Q, const void* K, const void* V, const void* O, const float* lse, const void* dO, void* dQ, void* dK,

@@ -79,6 +79,15 @@ def test_sizes(lib, B, Hq, Hkv, N, M, d):
         assert fwd >= 2 * 4 * B * Hq * N * (d + 1)
 
 
+@pytest.mark.parametrize("B,Hq,Hkv,N,M,d", [(8, 28, 4, 1, 1500, 128), (2, 8, 2, 40, 3000, 64), (1, 28, 4, 33, 65, 128)])
+def test_sizes_do_not_depend_on_strides(lib, B, Hq, Hkv, N, M, d):
+    """Heads of a group may be one run of rows or not: the workspace is enough for both."""
+    for dtype in (psa.PSA_BF16, psa.PSA_F32):
+        p = psa.make_params(B, Hq, Hkv, N, d, 128, 64, 4, dtype=dtype)
+        tokens = (N * Hq * d, d, Hq * d)
+        assert psa.psa_query_cross_sizes(p, M) == psa.psa_query_cross_sizes(p, psa.make_cross(M, q=tokens, o=tokens, dq=tokens, do=tokens))
+
+
 def test_oracle_gradients_are_differences():
     rng = np.random.default_rng(5)
     Q, dO = rng.standard_normal((1, 4, 3, 8)), rng.standard_normal((1, 4, 3, 8))
