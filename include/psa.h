@@ -141,7 +141,7 @@ int psa_permute_tokens(const psa_params* p, int32_t heads, const void* X, const 
  *   Qin, Qout   Q's two sides; both may be NULL: K alone.  Kin, Kout likewise.
  *   Qout == Qin (Kout == Kin) is allowed where both sides are contiguous and perm is NULL; other overlaps are not.
  *   Errors: PSA_EINVAL (null pointer, one side of a tensor without the other, pairing, axis, freq or strides out of range, in place
- *           otherwise), PSA_EUNSUPPORTED (2^31 rows or more), PSA_ELAUNCH.
+ *           otherwise, one tensor's output at the other's address), PSA_EUNSUPPORTED (2^31 rows or more), PSA_ELAUNCH.
  */
 enum { PSA_ROTARY_ADJACENT = 0, PSA_ROTARY_HALVES = 1 };
 #define PSA_ROTARY_MAX_AXES 4
@@ -303,7 +303,7 @@ int psa_dense_ref(const psa_params* p, const void* Q, const void* K, const void*
  *   contiguous [B, heads, N or M, d].  Not negative.  Inputs may repeat rows (stride 0, states that a batch shares); tensors that are written
  *   may not: ordered by size, each stride must reach past what the smaller ones cover.  From one token or state to the next at most
  *   32 MB.  The d*_stride are read by the backward call only, do_stride is dO's.
- *   M = 0 is allowed (K, V, dK, dV may then be NULL).
+ *   M = 0 is allowed (K, V, dK, dV may then be NULL).  What a call writes overlaps nothing else that it is given.
  * psa_query_cross_sizes (host call): bytes of workspace, either pointer may be NULL.  0 for most forward calls: only where few query
  *   rows meet many states do workgroups share a row's states and leave partial results there.  256-byte aligned.
  * psa_cross_attention_fwd
@@ -318,8 +318,8 @@ int psa_dense_ref(const psa_params* p, const void* Q, const void* K, const void*
  *   Memory of K, V that a batch shares (stride 0): dK, dV are each entry's own.
  * bfloat16: products on MFMA with fp32 accumulation; P and dS are rounded to bfloat16 for the products that consume them.  float32: fp32
  * products and sums.  No atomics: bit-reproducible.
- * Errors: PSA_EINVAL (null pointer, misaligned scratch, M < 0, causal, strides), PSA_EUNSUPPORTED (B * Hkv above 65535, Hq / Hkv * N or M
- *         above 2^31 - 129, strides above 32 MB), PSA_ELAUNCH.
+ * Errors: PSA_EINVAL (null pointer, misaligned scratch, M < 0, causal, strides, O, dQ, dK or dV at another tensor's address),
+ *         PSA_EUNSUPPORTED (B * Hkv above 65535, Hq / Hkv * N or M above 2^31 - 129, strides above 32 MB), PSA_ELAUNCH.
  */
 typedef struct psa_cross {
   int32_t M;

@@ -238,6 +238,7 @@ int psa_rotary(const psa_params* p, const psa_rotary_spec* r, const int32_t* pos
   Strides q = {0, 0, 0}, k = {0, 0, 0};
   if (Qin && !make_strides(r->q_stride, pl.B, pl.Hq, pl.N, pl.d, inverse != 0, &q)) return PSA_EINVAL;
   if (Kin && !make_strides(r->k_stride, pl.B, pl.Hkv, pl.N, pl.d, inverse != 0, &k)) return PSA_EINVAL;
+  if ((Qin && (Qout == Kin || Qout == Kout)) || (Kin && Kout == Qin)) return PSA_EINVAL;
   auto tight = [&](const Strides& x, int H) {
     return (x.n == pl.d || pl.N == 1) && (x.h == (int64_t)pl.N * pl.d || H == 1) && (x.b == (int64_t)H * pl.N * pl.d || pl.B == 1);
   };
@@ -408,24 +409,35 @@ int psa_attention_bwd(const psa_params* p, const void* Q, const void* K, const v
 }
 
 // ---- cross attention
-struct CrossLayout { size_t off_part, off_stats, fwd_bytes, off_D, off_dq, off_dk, off_dv, bwd_bytes; };
+// Workspace of a call, and how many workgroups share a row's states and a state's rows.
+struct CrossLayout { size_t off_part, off_stats, off_D, off_dq, off_dk, off_dv, bytes; };
 
-static CrossLayout cross_layout(const Plan& pl, int M) {
-  CrossLayout l;
-  const size_t rows = (size_t)pl.B * pl.Hq * pl.N, keys = (size_t)pl.B * pl.Hkv * M, e = sizeof(float);
-  const size_t kf = cross_key_parts(pl, M, false), kb = cross_key_parts(pl, M, true), rp = cross_row_parts(pl, M);
-  l.off_part = 0;
-  l.off_stats = kf > 1 ? align256(kf * rows * pl.d * e) : 0;
-  l.fwd_bytes = kf > 1 ? l.off_stats + align256(kf * rows * e) : 0;
+static CrossLayout cross_fwd_layout(const Plan& pl, CrossCall* c) {
+  CrossLayout l = {};
+  const size_t rows = (size_t)pl.B * pl.Hq * pl.N, e = sizeof(float), kp = c->key_parts = cross_key_parts(pl, c->M, false);
+  if (kp == 1) return l;
+  l.off_stats = align256(kp * rows * pl.d * e);
+  l.bytes = l.off_stats + align256(kp * rows * e);
+  return l;
+}
+static CrossLayout cross_bwd_layout(const Plan& pl, CrossCall* c) {
+  CrossLayout l = {};
+  const size_t rows = (size_t)pl.B * pl.Hq * pl.N, keys = (size_t)pl.B * pl.Hkv * c->M, e = sizeof(float);
+  const size_t kp = c->key_parts = cross_key_parts(pl, c->M, true), rp = c->row_parts = cross_row_parts(pl, c->M);
   size_t s = 0;
   l.off_D = s;  s += align256(2 * rows * e);
-  l.off_dq = s; s += kb > 1 ? align256(kb * rows * pl.d * e) : 0;
+  l.off_dq = s; s += kp > 1 ? align256(kp * rows * pl.d * e) : 0;
   l.off_dk = s; s += rp > 1 ? align256(rp * keys * pl.d * e) : 0;
   l.off_dv = s; s += rp > 1 ? align256(rp * keys * pl.d * e) : 0;
-  l.bwd_bytes = s;
+  l.bytes = s;
   return l;
 }
 
+static void merge_rows(Plan* pl) {
+  pl->N *= pl->group;
+  pl->Hq = pl->Hkv;
+  pl->group = 1;
+}
 // Query heads of a key head whose rows follow each other in equal steps (one token each, or contiguous heads) are one head of group * N tokens: fewer blocks of rows that are
 // partly empty, nothing to tell heads apart.
 static void merge_heads(Plan* pl, CrossCall* c, bool gradients) {
@@ -438,9 +450,7 @@ static void merge_heads(Plan* pl, CrossCall* c, bool gradients) {
     if (pl->N == 1) row_tensors[i]->n = row_tensors[i]->h;
     row_tensors[i]->h *= pl->group;
   }
-  pl->N *= pl->group;
-  pl->Hq = pl->Hkv;
-  pl->group = 1;
+  merge_rows(pl);
 }
 
 static int make_cross(const psa_params* p, const psa_cross* x, Plan* pl, CrossCall* c, bool gradients) {
@@ -466,14 +476,14 @@ int psa_query_cross_sizes(const psa_params* p, const psa_cross* x, size_t* fwd_s
   CrossCall c;
   const int rc = make_cross(p, x, &pl, &c, true);
   if (rc != PSA_OK) return rc;
+  auto most = [](size_t u, size_t v) { return u > v ? u : v; };
   // the same for all strides: with and without merged heads
-  CrossLayout l = cross_layout(pl, c.M);
-  pl.N *= pl.group;
-  pl.Hq = pl.Hkv;
-  pl.group = 1;
-  const CrossLayout m = cross_layout(pl, c.M);
-  if (fwd_scratch) *fwd_scratch = l.fwd_bytes > m.fwd_bytes ? l.fwd_bytes : m.fwd_bytes;
-  if (bwd_scratch) *bwd_scratch = l.bwd_bytes > m.bwd_bytes ? l.bwd_bytes : m.bwd_bytes;
+  for (int merged = 0; merged < (pl.group > 1 ? 2 : 1); ++merged) {
+    Plan one = pl;
+    if (merged) merge_rows(&one);
+    if (fwd_scratch) *fwd_scratch = most(merged ? *fwd_scratch : 0, cross_fwd_layout(one, &c).bytes);
+    if (bwd_scratch) *bwd_scratch = most(merged ? *bwd_scratch : 0, cross_bwd_layout(one, &c).bytes);
+  }
   return PSA_OK;
 }
 
@@ -483,10 +493,10 @@ int psa_cross_attention_fwd(const psa_params* p, const psa_cross* x, const void*
   CrossCall c;
   const int rc = make_cross(p, x, &pl, &c, false);
   if (rc != PSA_OK) return rc;
-  if (!Q || !O || (c.M > 0 && (!K || !V))) return PSA_EINVAL;
+  if (!Q || !O || (c.M > 0 && (!K || !V)) || O == Q || O == K || O == V) return PSA_EINVAL;
   merge_heads(&pl, &c, false);
-  const CrossLayout l = cross_layout(pl, c.M);
-  if (l.fwd_bytes && (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255))) return PSA_EINVAL;
+  const CrossLayout l = cross_fwd_layout(pl, &c);
+  if (l.bytes && (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255))) return PSA_EINVAL;
   c.kv_len = kv_len;
   c.key_mask = key_mask;
   return launch_cross_fwd(pl, c, Q, K, V, O, lse, reinterpret_cast<float*>(at(scratch, l.off_part)), reinterpret_cast<float*>(at(scratch, l.off_stats)),
@@ -502,8 +512,12 @@ int psa_cross_attention_bwd(const psa_params* p, const psa_cross* x, const void*
   if (rc != PSA_OK) return rc;
   if (!Q || !O || !lse || !dO || !dQ || !scratch || (c.M > 0 && (!K || !V || !dK || !dV))) return PSA_EINVAL;
   if (reinterpret_cast<uintptr_t>(scratch) & 255) return PSA_EINVAL;
+  const void* const tensors[8] = {dQ, dK, dV, Q, K, V, O, dO};
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 8; ++j)
+      if (tensors[i] && tensors[i] == tensors[j]) return PSA_EINVAL;       // (the kernel of dK and dV reads Q and dO after dQ is written)
   merge_heads(&pl, &c, true);
-  const CrossLayout l = cross_layout(pl, c.M);
+  const CrossLayout l = cross_bwd_layout(pl, &c);
   c.kv_len = kv_len;
   c.key_mask = key_mask;
   auto f = [&](size_t off) { return reinterpret_cast<float*>(at(scratch, off)); };

@@ -2,12 +2,9 @@
 // key_mask[b, j] != 0.  With s_j = scale q.k_j:  P = softmax over the states that are seen, O = P V, lse = log sum exp(s).  Backward, with
 // P = exp(s - lse), D = dO.O, dP = dO V^T, dS = P (dP - D):  dQ = scale dS K, dK = scale dS^T Q, dV = P^T dO.
 //
-// All three kernels are made of two products on 32x32 MFMA tiles with fp32 accumulation (see Mma):
-//   rows:  [32 rows of a tile in LDS] x [32 rows in registers]^T   -> one register row in each lane, the tile's rows in its registers
-//   cols:  [32 rows of a tile in LDS]^T x [that result]            -> the result is the second operand as it lies, no lane exchange
-// forward, dQ: the tile is a piece of K or V, the registers hold the query rows; dK, dV: the tile is a piece of Q or dO, the registers hold
-// keys and values.  The query heads of a key head are rows of one matrix (row = head in group * N + token), so that few tokens of many
-// heads fill a tile.  Tiles come straight into LDS, double buffered, one tile ahead; one barrier a tile.
+// The kernels of a type are in cross_bf16.hip and cross_f32.hip (what they share: cross_dev.h); here are those that add up partial results and the rules by which the
+// host shares the work.  Query rows stay in registers and tiles of states come by (forward, dQ), or states stay and tiles of query rows come by (dK, dV).  The query
+// heads of a key head are rows of one matrix where that fills tiles better (cross_flat; merge_heads in api.hip).
 // No atomics: sums over workgroups are written as partial results and added in a fixed order.
 #include "cross_dev.h"
 
@@ -110,6 +107,7 @@ static int cross_parts(int64_t blocks, int64_t tiles, const CrossCost& c, double
   int best = 1;
   double least = 0.0;
   for (int64_t p = 1; p <= 128 && p <= (tiles > 1 ? tiles : 1); ++p) {
+    if (p > 1 && c.lone + c.start + 5.0 + (double)p * part_bytes / 1.75e6 >= least) break;      // more parts take longer than the best
     const int64_t w = (blocks * p + 255) / 256, each = (tiles + p - 1) / p;
     const double us = (double)each * (w * c.busy > c.lone ? w * c.busy : c.lone) + (double)((w + c.fit - 1) / c.fit) * c.start + (p > 1 ? 5.0 + (double)p * part_bytes / 1.75e6 : 0.0);
     if (p == 1 || us < least) {
@@ -169,7 +167,7 @@ template <typename T>
 static void launch_cross_fwd_t(const Plan& pl, const CrossCall& c, const void* Q, const void* K, const void* V, void* O, float* lse, float* part, float* stats, hipStream_t s) {
   CrossArgs a = cross_args(pl, c);
   const int nw = cross_waves(pl);
-  cross_share(a, cross_key_parts(pl, c.M, false), (c.M + cross_keys<T>() - 1) / cross_keys<T>());
+  cross_share(a, c.key_parts, (c.M + cross_keys<T>() - 1) / cross_keys<T>());
   const bool split = a.parts > 1;
   T* o = static_cast<T*>(O);
   cross_fwd(a, pl.d, cross_row_grid(pl, a, nw), nw, split, static_cast<const T*>(Q), static_cast<const T*>(K), static_cast<const T*>(V), o, split ? stats : lse, part, s);
@@ -200,11 +198,11 @@ static void launch_cross_bwd_t(const Plan& pl, const CrossCall& c, const void* Q
     sums.of[tensors++] = {part, out, rows, to, H, L, a.parts, factor};
     if (rows > most) most = rows;
   };
-  cross_share(a, cross_key_parts(pl, c.M, true), (c.M + cross_keys<T>() - 1) / cross_keys<T>());
+  cross_share(a, c.key_parts, (c.M + cross_keys<T>() - 1) / cross_keys<T>());
   cross_dq(a, pl.d, cross_row_grid(pl, a, nw), nw, a.parts > 1, q, k, v, o, lse, g, Dr, gq, dQpart, s);
   if (a.parts > 1) add(dQpart, gq, pl.Hq, pl.N, c.gq, pl.scale);
   if (c.M > 0) {
-    cross_share(a, cross_row_parts(pl, c.M), pl.group * a.chunks);
+    cross_share(a, c.row_parts, pl.group * a.chunks);
     cross_dkv(a, pl.d, dim3((unsigned)((c.M + 127) / 128), (unsigned)(pl.B * pl.Hkv), (unsigned)a.parts), a.parts > 1, q, k, v, Dr, g, gk, gv, dKpart, dVpart, s);
     if (a.parts > 1) {
       add(dKpart, gk, pl.Hkv, c.M, c.gk, pl.scale);

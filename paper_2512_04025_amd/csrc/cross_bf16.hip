@@ -3,7 +3,7 @@
 
 namespace psa {
 
-// bfloat16: the same, with the order of a tile fixed by hand.  A step makes the scores of tile t + 1 and the second product of tile t, and every MFMA is
+// Forward.  A step makes the scores of tile t + 1 and the second product of tile t, and every MFMA is
 // followed by a slice of the vector work (exponentials of tile t, maximum of tile t + 1), about one weight a lane per MFMA, so that
 // one wavefront keeps both pipes busy; K is loaded a tile further ahead than V.
 template <int D, int NW, bool PART>

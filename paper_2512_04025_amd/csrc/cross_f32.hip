@@ -1,6 +1,6 @@
 // Cross attention and its gradients (see cross.hip), float32.
 //
-// The fp32 matrix instructions (32x32x2: 64 cycles each, 128 times slower than bfloat16's) bound every kernel here: 4096 cycles for 32 x 32 x 128 on a SIMD.  Operands
+// The fp32 matrix instructions (32x32x2: 64 cycles for 2 channels, bfloat16's 32 for 16: a sixteenth of the rate) bound every kernel here: 4096 cycles for 32 x 32 x 128 on a SIMD.  Operands
 // are requested a step ahead, and where two products share their shape their instructions take turns.  (Three bfloat16 planes of every operand, made from the tile
 // for each product, were slower: gradients of 12 heads x 1000 tokens x 301 states at d = 128 107 -> 132 us.)
 #include "cross_dev.h"

@@ -70,10 +70,11 @@ constexpr int ROTARY_PAIRS = 64;
 hipError_t launch_rotary(const Plan& pl, const psa_rotary_spec& r, int Hq, int Hkv, const Strides& q, const Strides& k, const int32_t* pos, int64_t pos_stride,
                          const int32_t* perm, bool inverse, const void* Qin, const void* Kin, void* Qout, void* Kout, hipStream_t s);
 void rotary_spectrum_host(int d, int axes, const int32_t* pairs, double base, bool shared, psa_rotary_spec* r);
-// Cross attention to M states.  part, stats / dQpart / dKpart, dVpart: partial results in fp32 (cross_key_parts or cross_row_parts times the
-// result's elements; unused where that is 1); Dr: two floats per query row.
+// Cross attention to M states.  part, stats / dQpart / dKpart, dVpart: partial results in fp32 (key_parts or row_parts times the result's
+// elements; unused where that is 1); Dr: two floats per query row.
 struct CrossCall {
   int M;
+  int key_parts, row_parts;                   // workgroups that share the states of a block of rows, the rows of a block of states
   Strides q, k, v, o, gq, gk, gv, go;         // g: the gradients
   const int32_t* kv_len;
   const uint8_t* key_mask;

@@ -66,6 +66,18 @@ def test_refusals_before_any_launch(lib):
         psa.psa_query_cross_sizes(p, -1)
 
 
+def test_outputs_at_another_tensors_address_are_refused(lib):
+    p = psa.make_params(2, 4, 2, 100, 64, 64, 64, 4)
+    x = psa.make_cross(50)
+    for other in ("Q", "K", "V"):
+        assert _fwd(lib, p, x, **{other: 1024}) == 1, other
+    at = dict(Q=256, K=512, V=768, O=1024, dO=1536, dQ=1792, dK=2048, dV=2304)
+    for out in ("dQ", "dK", "dV"):
+        for other in at:
+            if other != out:
+                assert _bwd(lib, p, x, **{out: at[other]}) == 1, (out, other)
+
+
 @pytest.mark.parametrize("B,Hq,Hkv,N,M,d", [(1, 12, 12, 32760, 512, 128), (1, 40, 40, 75600, 512, 128), (2, 4, 2, 100, 0, 64), (8, 28, 4, 1, 77, 128), (1, 1, 1, 1, 30000, 64), (2, 16, 16, 64, 32760, 64)])
 def test_sizes(lib, B, Hq, Hkv, N, M, d):
     p = psa.make_params(B, Hq, Hkv, N, d, 128, 64, 4)

@@ -152,6 +152,20 @@ def test_element_alignment(dtype, d, offset):
 
 
 @BOTH
+def test_offsets_beyond_32_bits(dtype, d):
+    """Rows 16 MB apart, 270 of them: every tensor ends 4.5 GB behind its first element."""
+    import torch
+    a = Problem(dtype, d, 1, 2, 2, 270, 261, lengths=[258])
+    esize = a.Q.element_size()
+    step = 2 ** 24 // esize
+    flat = torch.empty(270 * step, dtype=a.Q.dtype, device="cuda")
+    far = [flat.as_strided(x.shape, (270 * step, d, step, 1), i * 2 * d).copy_(x) for i, x in enumerate((a.Q, a.K, a.V, a.O, a.dO, *a.grads))]
+    a.Q, a.K, a.V, a.O, a.dO, a.grads = *far[:5], far[5:]
+    a.x = psa.make_cross(261, q=a.Q, k=a.K, v=a.V, o=a.O, do=a.dO, dq=a.grads[0], dk=a.grads[1], dv=a.grads[2])
+    a.check()
+
+
+@BOTH
 def test_scores_of_a_wide_range(dtype, d):
     """A softmax that one state takes, and a scale of the caller's."""
     Problem(dtype, d, 1, 2, 2, 70, 300, gain=20.0).check()

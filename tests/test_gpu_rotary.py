@@ -108,6 +108,30 @@ def test_element_alignment(dtype, offset):
         check(dtype, 64, offset // 2, (12, 10, 10), False, 2, 3, 1, 45, "tokens", False, inverse, False, offset=offset)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_offsets_beyond_32_bits(dtype):
+    """Tokens 16 MB apart, 270 of them: Q and K end 4.5 GB behind their first element."""
+    import torch
+    p = psa.make_params(1, 4, 2, 270, 64, 64, 64, 1, dtype=psa.PSA_BF16 if dtype == "bf16" else psa.PSA_F32)
+    near = [rows((1, h, 270, 64), dtype, "heads", h) for h in (4, 2)]
+    step = 2 ** 24 // near[0].element_size()
+    flat = torch.empty(270 * step, dtype=near[0].dtype, device="cuda")
+    far = [flat.as_strided(x.shape, (270 * step, 64, step, 1), i * 4 * 64).copy_(x) for i, x in enumerate(near)]
+    spec = psa.make_rotary(64, (12, 10, 10), q=far[0], k=far[1])
+    pos = torch.arange(3 * 270, dtype=torch.int32, device="cuda").view(3, 270)
+    perm = torch.arange(269, -1, -1, dtype=torch.int32, device="cuda")
+    out = [torch.empty_like(x) for x in near]
+    psa.psa_rotary(p, spec, pos, *far, *out, perm=perm)
+    for x, got in zip(near, out):
+        want, size = oracle(f64(x), pos[None].cpu().numpy(), spec, 64, False)
+        assert np.all(np.abs(f64(got) - want[:, :, ::-1]) <= limit(want, size, dtype)[:, :, ::-1])
+    given = [f64(x) for x in out]
+    psa.psa_rotary(p, spec, pos, *out, *far, perm=perm, inverse=True)
+    for x, got in zip(given, far):
+        want, size = oracle(x[:, :, ::-1], pos[None].cpu().numpy(), spec, 64, True)
+        assert np.all(np.abs(f64(got) - want) <= limit(want, size, dtype))
+
+
 def test_far_positions():
     """Angles of 10^7 radians on the fastest channel: the remainder is made in 64 bits (float32 would be off by half a radian)."""
     check("f32", 128, 0, (22, 21, 21), False, 1, 2, 2, 501, "heads", False, False, False, far=10 ** 7)

@@ -55,6 +55,8 @@ def test_refusals_before_any_launch(lib):
     assert _call(lib, p, ok(pairing=2)) == 1
     assert _call(lib, p, ok(), q=(512, 512), perm=256) == 1                          # in place and permuted
     assert _call(lib, p, ok(q=(25600, 64, 256)), q=(512, 512)) == 1                  # in place from another layout
+    for q, k in (((512, 2048), (2048, 4096)), ((512, 4096), (2048, 4096)), ((512, 1024), (2048, 512))):      # one tensor's output at the other's address
+        assert _call(lib, p, ok(), q=q, k=k) == 1
     for bad in (0, 5):
         r = ok()
         r.axes = bad
