@@ -316,8 +316,8 @@ int psa_dense_ref(const psa_params* p, const void* Q, const void* K, const void*
  *   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO;  query heads that share a key head add up.  Every element of dQ, dK, dV is written.
  *   O, lse      as the forward call gave them;  dO [B, Hq, N, d]
  *   Memory of K, V that a batch shares (stride 0): dK, dV are each entry's own.
- * bfloat16: products on MFMA with fp32 accumulation; P and dS are rounded to bfloat16 for the products that consume them.  float32: fp32
- * products and sums.  No atomics: bit-reproducible.
+ * bfloat16: products on MFMA with fp32 accumulation; P and dS are rounded to bfloat16 for the products that consume them; with few query rows to a
+ * key head to two bfloat16 numbers (2^-16): for dQ at most 64 of them, for dK and dV at most 32.  float32: fp32 products and sums.  No atomics: bit-reproducible.
  * Errors: PSA_EINVAL (null pointer, misaligned scratch, M < 0, causal, strides, O, dQ, dK or dV at another tensor's address),
  *         PSA_EUNSUPPORTED (B * Hkv above 65535, Hq / Hkv * N or M above 2^31 - 129, strides above 32 MB), PSA_ELAUNCH.
  */

@@ -221,15 +221,34 @@ __global__ __launch_bounds__(NW * 64, D == 64 ? 3 : 2) void cross_fwd_bf16_kerne
 
 // ---- bfloat16 gradients with the order of a tile fixed by hand: every operand fragment is requested two MFMAs ahead, and a slice of the vector work stands behind each MFMA.
 
+// A rounding of P or dS to bfloat16 costs a gradient about as much as its own rounding to bfloat16 does (of the norm: 0.0017 each, 0.0024 together).  Where many rows or states add up it
+// is one rounding.  Where few do, so that an outlying one can be most of the result (twice the error was seen), a second bfloat16 number holds what the first leaves over, and a second
+// product adds it: dQ with at most 64 query rows to a key head (less than four wavefronts), dK and dV with at most 32.  The matrix instructions are not what bounds the kernels there:
+// 2 x 16 heads x 64 rows x 8190 states, d = 64: dQ 17 -> 19 us; with dK and dV so too it would be 22 -> 29 us for these, hence 32.
+// What (x, y) leave over when rounded to the pair `bits`
+__device__ __forceinline__ uint32_t left_over(float x, float y, uint32_t bits) {
+  return f32_to_bf16_pair(x - __uint_as_float(bits << 16), y - __uint_as_float(bits & 0xffff0000u));
+}
+
 // 32 x 32 scores' fragments for the second products: pairs q = 0 .. 7 of registers 2q, 2q + 1
-struct WeightPairs {
-  uint32_t w[8];
+template <bool TWO> struct WeightPairs {
+  uint32_t w[8], rest[TWO ? 8 : 1];
   __device__ __forceinline__ void put(int q, float x, float y) {
     uint32_t bits = f32_to_bf16_pair(x, y);
     asm volatile("" : "+v"(bits));            // made here, not where it is used
     w[q] = bits;
+    if constexpr (TWO) {
+      bits = left_over(x, y, bits);
+      asm volatile("" : "+v"(bits));
+      rest[q] = bits;
+    }
   }
-  __device__ __forceinline__ bf16x8 frag(int f) const { return __builtin_bit_cast(bf16x8, (u32x4{w[4 * f], w[4 * f + 1], w[4 * f + 2], w[4 * f + 3]})); }
+  // acc + rows x weights 16 f .. 16 f + 15
+  template <typename X> __device__ __forceinline__ f32x16 mul(bf16x8 rows, int f, f32x16 acc) const {
+    acc = X::mul(rows, __builtin_bit_cast(bf16x8, (u32x4{w[4 * f], w[4 * f + 1], w[4 * f + 2], w[4 * f + 3]})), acc);
+    if constexpr (TWO) acc = X::mul(rows, __builtin_bit_cast(bf16x8, (u32x4{rest[4 * f], rest[4 * f + 1], rest[4 * f + 2], rest[4 * f + 3]})), acc);
+    return acc;
+  }
 };
 // The operand fragments that are on their way, by the slot that takes them: of rows (16 bytes a lane) or of columns (two transposing reads).  AGAIN: a fragment's
 // address is made for each request, where the compiler would hold those that come again over the tile.
@@ -360,7 +379,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cross_dq_bf16_kernel(const bf16_t*
     constexpr int HALF = 32 * X::ROWB, NF = 4 * KS + 4 * MD;
     Fragments<D, false> fr;
     f32x16 s[2], dp[2];
-    WeightPairs w[2];
+    WeightPairs<NW < 4> w[2];
     auto request = [&](auto tag) __attribute__((always_inline)) {
       constexpr int j = decltype(tag)::value;
       if constexpr (j < 4 * KS) fr.template row<j, j % KS>(tile + (j / KS & 1) * TILEB + j / (2 * KS) * HALF, rbase);
@@ -385,7 +404,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cross_dq_bf16_kernel(const bf16_t*
         else dp[u] = X::mul(fr.template get<j>(), gf[k], k == 0 ? ndot : dp[u]);
       } else {
         constexpr int u = (j - 4 * KS) / (2 * MD), c = (j - 4 * KS) % (2 * MD);
-        acc[c % MD] = X::mul(fr.template get<j>(), w[u].frag(c / MD), acc[c % MD]);
+        acc[c % MD] = w[u].template mul<X>(fr.template get<j>(), c / MD, acc[c % MD]);
       }
       if constexpr (j == KS || j == 3 * KS) {
         constexpr int u = j / (2 * KS);
@@ -427,8 +446,8 @@ __global__ __launch_bounds__(NW * 64, 2) void cross_dq_bf16_kernel(const bf16_t*
 }
 
 // dK, dV of 32 keys a wavefront.  Of 32 query rows: S, dP (beside the weights), the product for dV (beside dS), for dK.
-template <int D, bool PART>
-__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cross_dkv_bf16_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const float* __restrict__ stats,
+template <int D, bool PART, bool TWO>
+__global__ __launch_bounds__(256, D == 64 ? (TWO ? 2 : 3) : 2) void cross_dkv_bf16_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const float* __restrict__ stats,
                                                                 const bf16_t* __restrict__ dO, bf16_t* __restrict__ dK, bf16_t* __restrict__ dV, float* __restrict__ dKpart,
                                                                 float* __restrict__ dVpart, CrossArgs a) {
   typedef Mma<bf16_t, D> X;
@@ -513,7 +532,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cross_dkv_bf16_kernel(co
         const float* sl = stat + u * 32 + (lane_again() >> 5) * 4;
         Fragments<D, D == 128> fr;
         f32x16 s, dp;
-        WeightPairs w;
+        WeightPairs<TWO> w;
         f32x4 l[2];
         constexpr int NF = 2 * KS + 4 * MD;
         auto request = [&](auto tag) __attribute__((always_inline)) {
@@ -545,8 +564,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cross_dkv_bf16_kernel(co
           if constexpr (j == KS - 1) l[0] = *reinterpret_cast<const f32x4*>(sl);
           if constexpr (j < KS) s = X::mul(fr.template get<j>(), kf[j], j == 0 ? zero : s);
           else if constexpr (j < 2 * KS) dp = X::mul(fr.template get<j>(), vf[j - KS], dp);
-          else if constexpr (j < 2 * KS + 2 * MD) dv[(j - 2 * KS) % MD] = X::mul(fr.template get<j>(), w.frag((j - 2 * KS) / MD), dv[(j - 2 * KS) % MD]);
-          else dk[(j - 2 * KS) % MD] = X::mul(fr.template get<j>(), w.frag((j - 2 * KS - 2 * MD) / MD), dk[(j - 2 * KS) % MD]);
+          else if constexpr (j < 2 * KS + 2 * MD) dv[(j - 2 * KS) % MD] = w.template mul<X>(fr.template get<j>(), (j - 2 * KS) / MD, dv[(j - 2 * KS) % MD]);
+          else dk[(j - 2 * KS) % MD] = w.template mul<X>(fr.template get<j>(), (j - 2 * KS - 2 * MD) / MD, dk[(j - 2 * KS) % MD]);
           spread(tag, integral_constant<int, KS + 1>{}, integral_constant<int, 2 * KS>{}, integral_constant<int, 16>{}, [&](int e) __attribute__((always_inline)) {
             if (e % 4 == 0 && e < 12) l[(e / 4 + 1) & 1] = *reinterpret_cast<const f32x4*>(sl + (e / 4 + 1) * 8);
             float x = __builtin_amdgcn_exp2f(fmaf(s[e], a.scale_log2, l[(e / 4) & 1][e % 4]));
@@ -629,8 +648,14 @@ void cross_dq(const CrossArgs& a, int d, dim3 grid, int nw, bool part, const bf1
 void cross_dkv(const CrossArgs& a, int d, dim3 grid, bool part, const bf16_t* Q, const bf16_t* K, const bf16_t* V, const float* stats, const bf16_t* dO, bf16_t* dK, bf16_t* dV, float* dKpart,
                float* dVpart, hipStream_t s) {
   auto go = [&](auto kernel) { kernel<<<grid, 256, 0, s>>>(Q, K, V, stats, dO, dK, dV, dKpart, dVpart, a); };
-  if (d == 128) part ? go(cross_dkv_bf16_kernel<128, true>) : go(cross_dkv_bf16_kernel<128, false>);
-  else part ? go(cross_dkv_bf16_kernel<64, true>) : go(cross_dkv_bf16_kernel<64, false>);
+  const bool few = a.rows <= 32;
+  if (d == 128) {
+    if (few) part ? go(cross_dkv_bf16_kernel<128, true, true>) : go(cross_dkv_bf16_kernel<128, false, true>);
+    else part ? go(cross_dkv_bf16_kernel<128, true, false>) : go(cross_dkv_bf16_kernel<128, false, false>);
+  } else {
+    if (few) part ? go(cross_dkv_bf16_kernel<64, true, true>) : go(cross_dkv_bf16_kernel<64, false, true>);
+    else part ? go(cross_dkv_bf16_kernel<64, true, false>) : go(cross_dkv_bf16_kernel<64, false, false>);
+  }
 }
 
 }  // namespace psa

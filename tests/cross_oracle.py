@@ -16,6 +16,11 @@ def visible(B, M, kv_len, mask):
     return v
 
 
+def _weight_step(dtype, few):
+    """What is lost of a weight (P, dS) on its way into a product: bfloat16's half step; where few rows add up, that of a second number that holds the first's remainder."""
+    return 0.0 if dtype != "bf16" else HALF[dtype] ** 2 if few else HALF[dtype]
+
+
 def _scores(q, k, scale):
     """Scores and a bound of their error: d products and their sums in 32 bits, then the scale and the exponent's multiply-add."""
     s = q @ k.T * scale
@@ -24,12 +29,12 @@ def _scores(q, k, scale):
 
 
 def forward(Q, K, V, vis, scale, dtype):
-    """O, lse, and bounds of both. Weights are rounded to the type for the second product."""
+    """O, lse, and bounds of both. Weights are rounded for the second product."""
     B, Hq, N, d = Q.shape
     M = K.shape[2]
     O, lse = np.zeros((B, Hq, N, d)), np.full((B, Hq, N), -np.inf)
     bO, bl = np.zeros_like(O), np.zeros((B, Hq, N))
-    w = HALF[dtype] if dtype == "bf16" else 0.0
+    w = _weight_step(dtype, False)
     for b in range(B):
         j = np.nonzero(vis[b])[0]
         if len(j) == 0:
@@ -51,10 +56,11 @@ def forward(Q, K, V, vis, scale, dtype):
 
 
 def backward(Q, K, V, O, lse, dO, vis, scale, dtype):
-    """dQ, dK, dV from the outputs and statistics that the call is given, and their bounds. P and dS are rounded to the type where a product consumes them."""
+    """dQ, dK, dV from the outputs and statistics that the call is given, and their bounds. P and dS are rounded where a product consumes them."""
     B, Hq, N, d = Q.shape
     Hkv, M = K.shape[1], K.shape[2]
-    w, half = (HALF[dtype] if dtype == "bf16" else 0.0), HALF[dtype]
+    rows, half = Hq // Hkv * N, HALF[dtype]
+    wq, wk = _weight_step(dtype, rows <= 64), _weight_step(dtype, rows <= 32)
     dQ, dK, dV = np.zeros(Q.shape), np.zeros(K.shape), np.zeros(K.shape)
     bQ, bK, bV = np.zeros(Q.shape), np.zeros(K.shape), np.zeros(K.shape)
     terms = N * (Hq // Hkv) + 40
@@ -72,13 +78,14 @@ def backward(Q, K, V, O, lse, dO, vis, scale, dtype):
             dp, D = g @ v.T, (g * O[b, h]).sum(1, keepdims=True)
             edp = (d + 4) * U * (np.abs(g) @ np.abs(v).T + (np.abs(g) * np.abs(O[b, h])).sum(1, keepdims=True))
             ds = p * (dp - D)
-            eds = p * (np.abs(dp - D) * (2 * eps + 4 * U) + edp * (1 + 2 * eps)) + w * np.abs(ds) * (1 + 2 * eps)
+            eds = p * (np.abs(dp - D) * (2 * eps + 4 * U) + edp * (1 + 2 * eps))
+            edsq, edsk = (eds + w * np.abs(ds) * (1 + 2 * eps) for w in (wq, wk))
             dQ[b, h] = ds @ k * scale
-            bQ[b, h] = scale * ((eds + (M + 8) * U * np.abs(ds)) @ np.abs(k)) + half * np.abs(dQ[b, h])
+            bQ[b, h] = scale * ((edsq + (M + 8) * U * np.abs(ds)) @ np.abs(k)) + half * np.abs(dQ[b, h])
             dK[b, hk, j] += ds.T @ q * scale
-            bK[b, hk, j] += scale * ((eds + terms * U * np.abs(ds)).T @ np.abs(q))
+            bK[b, hk, j] += scale * ((edsk + terms * U * np.abs(ds)).T @ np.abs(q))
             dV[b, hk, j] += p.T @ g
-            bV[b, hk, j] += (p * (w + 2 * eps + terms * U)).T @ np.abs(g)
+            bV[b, hk, j] += (p * (wk + 2 * eps + terms * U)).T @ np.abs(g)
     bK += half * np.abs(dK)
     bV += half * np.abs(dV)
     return (dQ, dK, dV), tuple(1.01 * x + 1e-30 for x in (bQ, bK, bV))
