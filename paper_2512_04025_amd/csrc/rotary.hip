@@ -13,18 +13,21 @@ namespace psa {
 struct RotaryArgs {
   int N, Hq, Hkv, heads, groups, per_group;   // heads = Hq + Hkv; groups of per_group of them (the last may be short)
   uint32_t rows;                              // B * groups * N
+  int once;                                   // the inputs do not fit the memory-side cache
   int64_t pos_stride;
   Strides q, k;                               // the projections' side
   double quarters[ROTARY_PAIRS];              // quarter turns a position
   uint8_t axis[ROTARY_PAIRS];                 // 255: the pair is not turned
 };
 
-// Cosine and sine of pos * quarters quarter turns.  The product and what is left of it after whole quarters in 64 bits (position 10^6 on the
-// fastest channel is 6 10^5 quarters, of which 32 bits would keep 1/16), then Taylor's series on +- pi / 4: the first terms left out are below 2^-29.
+// Cosine and sine of pos * quarters quarter turns.  The whole quarters and what is left over in 64 bits (position 10^6 on the fastest channel is 6 10^5 quarters, of which 32 bits
+// would keep 1/16): at 1.5 2^52 a sum is rounded to a whole number, whose last bits it holds (|pos * quarters| < 2^51).  Then Taylor's series on +- pi / 4: the
+// first terms left out are below 2^-29.
 __device__ __forceinline__ void cos_sin(double quarters, int pos, float& c, float& s) {
-  const double x = quarters * (double)pos, whole = rint(x);
-  const int n = (int)(whole - 4.0 * floor(whole * 0.25));
-  const float a = (float)(x - whole) * 1.57079632679489661923f, a2 = a * a;
+  constexpr double WHOLE = 6755399441055744.0;
+  const double turned = fma(quarters, (double)pos, WHOLE), whole = turned - WHOLE;
+  const int n = (int)(__double_as_longlong(turned) & 3);
+  const float a = (float)fma(quarters, (double)pos, -whole) * 1.57079632679489661923f, a2 = a * a;
   const float sn = fmaf(a * a2, fmaf(a2, fmaf(a2, fmaf(a2, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), a);
   const float cs = fmaf(a2, fmaf(a2, fmaf(a2, fmaf(a2, fmaf(a2, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
   c = n & 1 ? sn : cs;
@@ -33,10 +36,15 @@ __device__ __forceinline__ void cos_sin(double quarters, int pos, float& c, floa
   if (n >= 2) s = -s;
 }
 
-// 16 bytes at any element's address.  Stores are non-temporal, loads are not: what is written does not push out of the memory-side cache what is still to be
-// read (12 + 12 heads x 32760 tokens, permuted, us: neither 86.5, both 78, loads alone 73, stores alone 62; x 4000 tokens 12.9 / 15.6 / 15.3 / 11.4).
+// 16 bytes at any element's address.  Stores are non-temporal, so that what is written does not push out of the memory-side cache (256 MB) what a projection left
+// there; loads are where the inputs do not fit it (12 + 12 heads x 32760 tokens, 201 MB, permuted, us, inputs in the cache / in memory: neither - / 80.7, stores
+// 62 / 75, both 73 / 73.6; 1.5 GB, inverse: 580 -> 572).
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
-template <typename T> __device__ __forceinline__ u32x4 load16(const T* p) { return *reinterpret_cast<const u32x4_any*>(p); }
+template <bool ONCE, typename T> __device__ __forceinline__ u32x4 load16(const T* p) {
+  const u32x4_any* q = reinterpret_cast<const u32x4_any*>(p);
+  if constexpr (ONCE) return __builtin_nontemporal_load(q);
+  else return *q;
+}
 template <typename T> __device__ __forceinline__ void store16(T* p, u32x4 v) { __builtin_nontemporal_store(v, reinterpret_cast<u32x4_any*>(p)); }
 
 // HALVES: pair i is channels i, i + d / 2, and a thread has a chunk of each half; otherwise channels 2i, 2i + 1 and one chunk.
@@ -55,16 +63,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const T* __restrict__ Qin, 
     t = perm[k];
     if ((uint32_t)t >= (uint32_t)a.N) return;
   }
-  float cs[PAIRS], sn[PAIRS];
-  uint32_t still = 0u;
-#pragma unroll
-  for (int u = 0; u < PAIRS; ++u) {
-    const int ax = a.axis[c * PAIRS + u];
-    still |= (uint32_t)(ax == 255) << u;
-    cos_sin(a.quarters[c * PAIRS + u], pos[b * a.pos_stride + (int64_t)(ax == 255 ? 0 : ax) * a.N + t], cs[u], sn[u]);
-    if (INVERSE) sn[u] = -sn[u];
-  }
-  const int first = HALVES ? c * VEC : c * VEC, second = D / 2 + c * VEC;
+  const int first = c * VEC, second = D / 2 + c * VEC;
   const int64_t tight_q = (int64_t)b * a.Hq * a.N + k, tight_k = (int64_t)b * a.Hkv * a.N + k;
   const int64_t loose_q = b * a.q.b + t * a.q.n, loose_k = b * a.k.b + t * a.k.n;
   auto place = [&](int h, const T*& src, T*& dst) __attribute__((always_inline)) {
@@ -74,16 +73,42 @@ __global__ __launch_bounds__(256) void rotary_kernel(const T* __restrict__ Qin, 
     src = (is_q ? Qin : Kin) + (INVERSE ? tight : loose);
     dst = (is_q ? Qout : Kout) + (INVERSE ? loose : tight);
   };
-  for (int h = h0; h < h1; h += AHEAD) {
-    u32x4 v[AHEAD][HALVES ? 2 : 1];
-    T* dst[AHEAD];
+  u32x4 v[AHEAD][HALVES ? 2 : 1];
+  T* dst[AHEAD];
+  auto load_as = [&](auto once, int h) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       const T* src;
       place(h + u < h1 ? h + u : h1 - 1, src, dst[u]);
-      v[u][0] = load16(src + first);
-      if (HALVES) v[u][HALVES ? 1 : 0] = load16(src + second);
+      v[u][0] = load16<decltype(once)::value>(src + first);
+      if (HALVES) v[u][HALVES ? 1 : 0] = load16<decltype(once)::value>(src + second);
     }
+  };
+  auto load = [&](int h) __attribute__((always_inline)) {
+    if (a.once) load_as(std::integral_constant<bool, true>{}, h);
+    else load_as(std::integral_constant<bool, false>{}, h);
+  };
+  // The angles are worked out while the first rows are on their way: what they need is requested before (12 + 12 heads x 32760 tokens 84 -> 75 us; inverse
+  // calls, whose scattered side is the written one, gain nothing and lose 2 % of the largest pass).
+  int at[PAIRS];
+  double quarters[PAIRS];
+  uint32_t still = 0u;
+#pragma unroll
+  for (int u = 0; u < PAIRS; ++u) {
+    const int ax = a.axis[c * PAIRS + u];
+    still |= (uint32_t)(ax == 255) << u;
+    quarters[u] = a.quarters[c * PAIRS + u];
+    at[u] = pos[b * a.pos_stride + (int64_t)(ax == 255 ? 0 : ax) * a.N + t];
+  }
+  if (!INVERSE) load(h0);
+  float cs[PAIRS], sn[PAIRS];
+#pragma unroll
+  for (int u = 0; u < PAIRS; ++u) {
+    cos_sin(quarters[u], at[u], cs[u], sn[u]);
+    if (INVERSE) sn[u] = -sn[u];
+  }
+  for (int h = h0; h < h1; h += AHEAD) {
+    if (INVERSE || h > h0) load(h);
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       if (h + u >= h1) break;
@@ -110,13 +135,14 @@ template <typename T, int D>
 static void launch_rotary_t(RotaryArgs& a, int B, bool halves, bool inverse, const void* Qin, const void* Kin, void* Qout, void* Kout, const int32_t* pos,
                             const int32_t* perm, hipStream_t s) {
   const int lanes = D / 2 / (halves ? Elem<T>::VEC : Elem<T>::VEC / 2), per_block = 256 / lanes;
-  // Heads a thread: as many as leave four workgroups to a compute unit, at most 4 (8: the largest pass 605 us instead of 585, the others the same).
+  // Heads a thread: as many as leave four workgroups to a compute unit, at most 4 (us at 2 / 4 / 8: 12 + 12 heads x 32760 tokens 93 / 75 / 76, the largest pass 631 / 580 / 598).
   const int64_t all = (int64_t)B * a.heads * a.N / per_block;
   int per = 1;
   while (per < 4 && per < a.heads && all / (2 * per) >= 1024) per *= 2;
   a.per_group = per;
   a.groups = (a.heads + per - 1) / per;
   a.rows = (uint32_t)((int64_t)B * a.groups * a.N);
+  a.once = (int64_t)B * a.heads * a.N * D * (int64_t)sizeof(T) > ((int64_t)256 << 20);
   const unsigned grid = (unsigned)((a.rows + (int64_t)per_block - 1) / per_block);
   auto go = [&](auto kernel) {
     kernel<<<grid, 256, 0, s>>>(static_cast<const T*>(Qin), static_cast<const T*>(Kin), static_cast<T*>(Qout), static_cast<T*>(Kout), pos, perm, a);
