@@ -150,7 +150,7 @@ static CrossArgs cross_args(const Plan& pl, const CrossCall& c) {
   a.kv_len = c.kv_len; a.mask = c.key_mask;
   a.chunks = (pl.N + cross_tile(pl) - 1) / cross_tile(pl);
   a.flat = cross_flat(pl);
-  a.parts = a.tiles_per_part = 0;
+  a.once = a.parts = a.tiles_per_part = 0;
   return a;
 }
 static void cross_share(CrossArgs& a, int parts, int tiles) {
@@ -169,8 +169,13 @@ static void launch_cross_fwd_t(const Plan& pl, const CrossCall& c, const void* Q
   const int nw = cross_waves(pl);
   cross_share(a, c.key_parts, (c.M + cross_keys<T>() - 1) / cross_keys<T>());
   const bool split = a.parts > 1;
+  const dim3 grid = cross_row_grid(pl, a, nw);
+  // Keys, values and partial results that do not fit the memory-side cache (256 MB) together: reading them past it costs what is still there and saves the writing back.  2 x 16 heads
+  // x 64 rows, d = 64, us with / without, states last used long ago: 134 MB 39 / 43, 268 MB 64 / 71, 402 MB 87 / 93; just used: 40 / 34, 64 / 57, 87 / 93.
+  // (Not in the backward call, whose kernels both read keys and values: 8190 states 52 / 46.)
+  a.once = grid.x == 1 && pl.esize * 2 * (int64_t)pl.B * pl.Hkv * c.M * pl.d + 4 * (int64_t)a.parts * pl.B * pl.Hq * pl.N * pl.d > ((int64_t)256 << 20);
   T* o = static_cast<T*>(O);
-  cross_fwd(a, pl.d, cross_row_grid(pl, a, nw), nw, split, static_cast<const T*>(Q), static_cast<const T*>(K), static_cast<const T*>(V), o, split ? stats : lse, part, s);
+  cross_fwd(a, pl.d, grid, nw, split, static_cast<const T*>(Q), static_cast<const T*>(K), static_cast<const T*>(V), o, split ? stats : lse, part, s);
   if (!split) return;
   const unsigned blocks = cross_rows_of_256((int64_t)pl.B * pl.Hq * pl.N, pl.d);
   if (pl.d == 128) cross_join_kernel<T, 128><<<blocks, 256, 0, s>>>(part, stats, o, lse, a);

@@ -27,7 +27,8 @@ __global__ __launch_bounds__(NW * 64, D == 64 ? 3 : 2) void cross_fwd_bf16_kerne
     const int have = len - (t0 + i) * BN;
     return have >= 64 ? ~0ull : (1ull << have) - 1ull;
   };
-  if (n > 0) ks.next(lds, wave);
+  const bool once = NW < 4 && a.once != 0;
+  if (n > 0) ks.next(lds, wave, once);
   int byte = byte_of(0), byte_next = byte_of(1);
 
   // the wavefront's rows: of one head, or (flat) the next 32 of the key head's rows
@@ -53,8 +54,8 @@ __global__ __launch_bounds__(NW * 64, D == 64 ? 3 : 2) void cross_fwd_bf16_kerne
     for (int v = 0; v < 16; ++v) acc[md][v] = 0.f;
   float m_run = -INFINITY, l_run = 0.f, shift = 0.f;
   if (n > 0) {
-    vs.next(lds + OFF_V, wave);
-    if (n > 1) ks.next(lds + TILEB, wave);
+    vs.next(lds + OFF_V, wave, once);
+    if (n > 1) ks.next(lds + TILEB, wave, once);
     const uint32_t rbase = rows_base<bf16_t, D>(lane), cbase = X::cols_base(lane);
     uint64_t seen = seen_of(byte, 0), seen_next = 0;
     auto advance = [&](float top) __attribute__((always_inline)) {
@@ -96,8 +97,8 @@ __global__ __launch_bounds__(NW * 64, D == 64 ? 3 : 2) void cross_fwd_bf16_kerne
       if (MORE) {
         seen_next = seen_of(byte_next, i + 1);
         byte_next = byte_of(i + 2);
-        if (i + 2 < n) ks.next(lds + PAR * TILEB, wave);
-        vs.next(lds + OFF_V + (PAR ^ 1) * TILEB, wave);
+        if (i + 2 < n) ks.next(lds + PAR * TILEB, wave, once);
+        vs.next(lds + OFF_V + (PAR ^ 1) * TILEB, wave, once);
       }
       unsigned char* vt = smem + OFF_V + PAR * TILEB;
       if (seen != ~0ull) {

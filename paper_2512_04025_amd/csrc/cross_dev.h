@@ -11,6 +11,7 @@ struct CrossArgs {
   int B, Hq, Hkv, group, N, M;
   int rows;                                   // group * N: query rows of a key head
   int flat;                                   // a block of rows may hold rows of several heads
+  int once;                                   // forward: the keys and values are read by one workgroup each and do not fit the memory-side cache
   int parts, tiles_per_part;                  // workgroups that share a row's keys (forward, dQ) or a key's rows (dK, dV)
   int chunks;                                 // dK, dV: tiles of one head's tokens
   float scale, scale_log2;
@@ -146,11 +147,15 @@ template <typename T, int D, int R, int NW> struct TileStream {
 #pragma unroll
     for (int k = 0; k < OFFS; ++k) off[k] = Stage<T, D, R, NW>::lane_offset(k, wave, lane_again(), step);
   }
-  __device__ __forceinline__ void next(uint32_t to, int wave) {       // `left` > 0
+  __device__ __forceinline__ void next(uint32_t to, int wave, bool once = false) {       // `left` > 0
     const rsrc_words rsrc = make_rsrc((const void*)base, (uint32_t)((left < R ? left : R) - 1) * step + X::ROWB);
+    auto load = [&](auto&& from) __attribute__((always_inline)) {
 #pragma unroll
-    for (int k = 0; k < NI; ++k)
-      load_lds16(rsrc, to + (uint32_t)((k * NW + wave) * RPI * X::ROWB), off[k % OFFS], (int)((uint32_t)((k * NW + wave) * RPI) * step));
+      for (int k = 0; k < NI; ++k)
+        from(rsrc, to + (uint32_t)((k * NW + wave) * RPI * X::ROWB), off[k % OFFS], (int)((uint32_t)((k * NW + wave) * RPI) * step));
+    };
+    if (once) load(load_lds16_once);
+    else load(load_lds16);
     base += (uint64_t)R * step;
     left -= R;
   }

@@ -131,6 +131,10 @@ typedef __attribute__((ext_vector_type(4))) uint32_t rsrc_words;
 __device__ __forceinline__ void load_lds16(const rsrc_words& rsrc, uint32_t to, int v, int s) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(v), "s"(rsrc), "s"(s) : "memory", "m0");
 }
+// the same for what is read once and does not fit the memory-side cache
+__device__ __forceinline__ void load_lds16_once(const rsrc_words& rsrc, uint32_t to, int v, int s) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds" ::"s"(to), "v"(v), "s"(rsrc), "s"(s) : "memory", "m0");
+}
 __device__ __forceinline__ void load_lds4(const rsrc_words& rsrc, uint32_t to, int v, int s) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(to), "v"(v), "s"(rsrc), "s"(s) : "memory", "m0");
 }

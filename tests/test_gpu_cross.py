@@ -165,6 +165,25 @@ def test_offsets_beyond_32_bits(dtype, d):
     a.check()
 
 
+def test_states_beyond_the_cache():
+    """A row or three against 300 MB of states, lengths that end in the last part: against 64 bits on the GPU, a head at a time."""
+    import torch
+    H, N, M, d, length = 2, 3, 300000, 128, 299990
+    p = params("bf16", 1, H, H, N, d)
+    Q, K, V = (torch.randn((1, H, n, d), generator=torch.Generator("cuda").manual_seed(n + i), device="cuda").to(torch.bfloat16) for i, n in ((1, N), (2, M), (3, M)))
+    O, lse = torch.empty_like(Q), torch.empty((1, H, N), device="cuda")
+    x = psa.make_cross(M)
+    psa.psa_cross_attention_fwd(p, x, Q, K, V, O, scratch(psa.psa_query_cross_sizes(p, x)[0]), lse=lse, kv_len=torch.tensor([length], dtype=torch.int32, device="cuda"))
+    for h in range(H):
+        q, k, v = Q[0, h].double(), K[0, h, :length].double(), V[0, h, :length].double()
+        s = q @ k.t().contiguous() / math.sqrt(d)
+        w = torch.softmax(s, 1)
+        # 128 products and a scale in 32 bits are the error of a score, the states' sums that of the rest; weights and outputs are rounded to bfloat16
+        delta = 2.0 ** -24 * ((d + 4) * (q.abs() @ k.abs().t().contiguous()).max() / math.sqrt(d) + 8 * (1 + s.abs().max()))
+        assert torch.all((lse[0, h].double() - torch.logsumexp(s, 1)).abs() <= delta + (M + 60) * 2.0 ** -24)
+        assert torch.all((O[0, h].double() - w @ v).abs() <= 1.01 * ((w @ v.abs()) * (2.0 ** -8 + 2 * delta + (M + 8) * 2.0 ** -24) + 2.0 ** -8 * (w @ v).abs()))
+
+
 @BOTH
 def test_scores_of_a_wide_range(dtype, d):
     """A softmax that one state takes, and a scale of the caller's."""

@@ -132,6 +132,23 @@ def test_offsets_beyond_32_bits(dtype):
         assert np.all(np.abs(f64(got) - want) <= limit(want, size, dtype))
 
 
+@pytest.mark.parametrize("pairing,inverse", [(0, False), (1, True)])
+def test_inputs_beyond_the_cache_have_the_bits_of_their_parts(pairing, inverse):
+    """276 MB of rows in one call, and a part of the tokens at a time."""
+    import torch
+    B, H, N, d = 1, 12, 45000, 128
+    Q, K = (torch.randn((B, H, N, d), generator=torch.Generator("cuda").manual_seed(i), device="cuda").to(torch.bfloat16) for i in (1, 2))
+    pos = torch.randint(-5000, 5000, (3, N), generator=torch.Generator("cuda").manual_seed(3), device="cuda", dtype=torch.int32)
+    whole = [torch.empty_like(x) for x in (Q, K)]
+    psa.psa_rotary(psa.make_params(B, H, H, N, d, 64, 64, 1), psa.make_rotary(d, (22, 21, 21), pairing=pairing), pos, Q, K, *whole, inverse=inverse)
+    for at in (0, 20000, 40000):
+        n = min(20000, N - at)
+        part = [x[:, :, at:at + n].contiguous() for x in (Q, K)]
+        out = [torch.empty_like(x) for x in part]
+        psa.psa_rotary(psa.make_params(B, H, H, n, d, 64, 64, 1), psa.make_rotary(d, (22, 21, 21), pairing=pairing), pos[:, at:at + n].contiguous(), *part, *out, inverse=inverse)
+        assert all(torch.equal(x[:, :, at:at + n], y) for x, y in zip(whole, out))
+
+
 def test_far_positions():
     """Angles of 10^7 radians on the fastest channel: the remainder is made in 64 bits (float32 would be off by half a radian)."""
     check("f32", 128, 0, (22, 21, 21), False, 1, 2, 2, 501, "heads", False, False, False, far=10 ** 7)
