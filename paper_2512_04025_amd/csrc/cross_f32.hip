@@ -185,25 +185,15 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void cross_fwd_f32_kernel
   }
   const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
   const float stat = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * CROSS_LN2;
-  if constexpr (PART) {
-    if (!k.active) return;
-    const int64_t at = ((int64_t)k.part * a.B * a.Hkv + k.bh) * a.rows + k.row;
-    float* po = Opart + at * D;
-#pragma unroll
-    for (int md = 0; md < X::MD; ++md)
-#pragma unroll
-      for (int g4 = 0; g4 < 4; ++g4)
-        *reinterpret_cast<f32x4*>(po + md * 32 + g4 * 8 + hf * 4) = f32x4{acc[md][g4 * 4], acc[md][g4 * 4 + 1], acc[md][g4 * 4 + 2], acc[md][g4 * 4 + 3]} * inv;
-    if (hf == 0) lse[at] = stat;
-  } else {
-    if (lse && k.active && hf == 0) lse[((int64_t)k.b * a.Hq + k.hk * a.group) * a.N + k.row] = stat;
-    lds_ready();                              // everyone has read the last tile
-    rows_out<float, D>(acc, inv, smem + k.wave * 32 * X::ROWB, lane, [&](int r) __attribute__((always_inline)) -> float* {
-      if (k.row0 + r >= a.rows) return nullptr;
-      const CrossRow c = cross_row(a, k.row0 + r);
-      return O + k.b * a.o.b + (int64_t)(k.hk * a.group + c.g) * a.o.h + c.n * a.o.n;
-    });
-  }
+  const int64_t at = ((int64_t)k.part * a.B * a.Hkv + k.bh) * a.rows + k.row0;
+  if (lse && k.active && hf == 0) lse[PART ? at + (lane & 31) : ((int64_t)k.b * a.Hq + k.hk * a.group) * a.N + k.row] = stat;
+  lds_ready();                                // everyone has read the last tile
+  rows_out<float, D>(acc, inv, smem + k.wave * 32 * X::ROWB, lane, [&](int r) __attribute__((always_inline)) -> float* {
+    if (k.row0 + r >= a.rows) return nullptr;
+    if constexpr (PART) return Opart + (at + r) * D;
+    const CrossRow c = cross_row(a, k.row0 + r);
+    return O + k.b * a.o.b + (int64_t)(k.hk * a.group + c.g) * a.o.h + c.n * a.o.n;
+  });
 }
 
 // dQ of 32 rows a wavefront; and for the kernel after it -D, D = dO.O, and -lse log2(e) of every row (parts: the first one's)
@@ -220,17 +210,14 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && D == 64 ? 2 : 1) void cross_dq_
   const int head = k.hk * a.group + r.g;
   const int64_t stat_at = ((int64_t)k.b * a.Hq + k.hk * a.group) * a.N + k.row;
   RowSide<D> q, g;
-  q.load(Q + k.b * a.q.b + (int64_t)head * a.q.h + r.n * a.q.n, lane, k.active);
-  g.load(dO + k.b * a.go.b + (int64_t)head * a.go.h + r.n * a.go.n, lane, k.active);
   float dot = 0.f;
-  if (k.active) {
-    const float* gp = dO + k.b * a.go.b + (int64_t)head * a.go.h + r.n * a.go.n;
-    const float* op = O + k.b * a.o.b + (int64_t)head * a.o.h + r.n * a.o.n;
-#pragma unroll 4
-    for (int c = hf * 4; c < D; c += 8) {
-      const f32x4 x = Four<float>::load(op + c), y = Four<float>::load(gp + c);
-      dot += fmaf(x[0], y[0], x[1] * y[1]) + fmaf(x[2], y[2], x[3] * y[3]);
-    }
+  {
+    RowSide<D> o;
+    g.load(dO + k.b * a.go.b + (int64_t)head * a.go.h + r.n * a.go.n, lane, k.active);
+    o.load(O + k.b * a.o.b + (int64_t)head * a.o.h + r.n * a.o.n, lane, k.active);
+    q.load(Q + k.b * a.q.b + (int64_t)head * a.q.h + r.n * a.q.n, lane, k.active);
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c) dot += fmaf(o.f[c][0], g.f[c][0], o.f[c][1] * g.f[c][1]) + fmaf(o.f[c][2], g.f[c][2], o.f[c][3] * g.f[c][3]);
   }
   {
     float x, y;
@@ -263,22 +250,13 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && D == 64 ? 2 : 1) void cross_dq_
     for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], a.scale_log2, shift)) * (dp[v] - dot);
     cols<D>(acc, tile, lane, s);
   }
-  if constexpr (PART) {
-    if (!k.active) return;
-    float* po = dQpart + (((int64_t)k.part * a.B * a.Hkv + k.bh) * a.rows + k.row) * D;
-#pragma unroll
-    for (int md = 0; md < X::MD; ++md)
-#pragma unroll
-      for (int g4 = 0; g4 < 4; ++g4)
-        *reinterpret_cast<f32x4*>(po + md * 32 + g4 * 8 + hf * 4) = f32x4{acc[md][g4 * 4], acc[md][g4 * 4 + 1], acc[md][g4 * 4 + 2], acc[md][g4 * 4 + 3]};
-  } else {
-    lds_ready();
-    rows_out<float, D>(acc, a.scale, smem + k.wave * 32 * X::ROWB, lane, [&](int x) __attribute__((always_inline)) -> float* {
-      if (k.row0 + x >= a.rows) return nullptr;
-      const CrossRow c = cross_row(a, k.row0 + x);
-      return dQ + k.b * a.gq.b + (int64_t)(k.hk * a.group + c.g) * a.gq.h + c.n * a.gq.n;
-    });
-  }
+  lds_ready();                                // everyone has read the last tile
+  rows_out<float, D>(acc, PART ? 1.f : a.scale, smem + k.wave * 32 * X::ROWB, lane, [&](int x) __attribute__((always_inline)) -> float* {
+    if (k.row0 + x >= a.rows) return nullptr;
+    if constexpr (PART) return dQpart + (((int64_t)k.part * a.B * a.Hkv + k.bh) * a.rows + k.row0 + x) * D;
+    const CrossRow c = cross_row(a, k.row0 + x);
+    return dQ + k.b * a.gq.b + (int64_t)(k.hk * a.group + c.g) * a.gq.h + c.n * a.gq.n;
+  });
 }
 
 // dK, dV of 32 keys a wavefront: the query rows of the key's group, a head after the other, in tiles of 32 tokens
@@ -352,39 +330,21 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void cross_dkv_f32_kernel(con
     cols<D>(dv, tile + TILEB, lane, s);
     cols<D>(dk, tile, lane, g);
   }
-  if constexpr (PART) {
-    if (key >= a.M) return;
-    const int64_t to = (((int64_t)part * a.B * a.Hkv + bh) * a.M + key) * D;
+  if (!seen) {
 #pragma unroll
     for (int md = 0; md < X::MD; ++md)
 #pragma unroll
-      for (int g4 = 0; g4 < 4; ++g4) {
-        const int c = md * 32 + g4 * 8 + hf * 4;
-        f32x4 x, y;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[e] = seen ? dk[md][g4 * 4 + e] : 0.f;
-          y[e] = seen ? dv[md][g4 * 4 + e] : 0.f;
-        }
-        *reinterpret_cast<f32x4*>(dKpart + to + c) = x;
-        *reinterpret_cast<f32x4*>(dVpart + to + c) = y;
-      }
-  } else {
-    if (!seen) {
-#pragma unroll
-      for (int md = 0; md < X::MD; ++md)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) dk[md][v] = dv[md][v] = 0.f;
-    }
-    lds_ready();
-    unsigned char* mine = smem + wave * 32 * X::ROWB;
-    rows_out<float, D>(dk, a.scale, mine, lane, [&](int x) __attribute__((always_inline)) -> float* {
-      return key0 + x < a.M ? dK + b * a.gk.b + hk * a.gk.h + (int64_t)(key0 + x) * a.gk.n : nullptr;
-    });
-    rows_out<float, D>(dv, 1.f, mine, lane, [&](int x) __attribute__((always_inline)) -> float* {
-      return key0 + x < a.M ? dV + b * a.gv.b + hk * a.gv.h + (int64_t)(key0 + x) * a.gv.n : nullptr;
-    });
+      for (int v = 0; v < 16; ++v) dk[md][v] = dv[md][v] = 0.f;
   }
+  lds_ready();
+  unsigned char* rows_of = smem + wave * 32 * X::ROWB;
+  const int64_t to = (((int64_t)part * a.B * a.Hkv + bh) * a.M + key0) * D;
+  rows_out<float, D>(dk, PART ? 1.f : a.scale, rows_of, lane, [&](int x) __attribute__((always_inline)) -> float* {
+    return key0 + x >= a.M ? nullptr : PART ? dKpart + to + x * D : dK + b * a.gk.b + hk * a.gk.h + (int64_t)(key0 + x) * a.gk.n;
+  });
+  rows_out<float, D>(dv, 1.f, rows_of, lane, [&](int x) __attribute__((always_inline)) -> float* {
+    return key0 + x >= a.M ? nullptr : PART ? dVpart + to + x * D : dV + b * a.gv.b + hk * a.gv.h + (int64_t)(key0 + x) * a.gv.n;
+  });
 }
 
 template <int D> static void fwd_d(const CrossArgs& a, dim3 grid, int nw, bool part, const float* Q, const float* K, const float* V, float* O, float* lse, float* Opart, hipStream_t s) {
