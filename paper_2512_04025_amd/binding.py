@@ -392,6 +392,7 @@ def psa_cross_attention_fwd(p: PsaParams, x: PsaCross, Q, K, V, O, scratch=None,
 
 
 def psa_cross_attention_bwd(p: PsaParams, x: PsaCross, Q, K, V, O, lse, dO, dQ, dK, dV, scratch, kv_len=None, key_mask=None, stream=None) -> None:
+    """O, lse: as the forward call gave them; dO: as O; dQ, dK, dV: as Q, K, V, all written."""
     lib, torch, dev, at, dt = _here(p, stream)
     B, Hq, N, d = p.B, p.Hq, p.N, p.d
     sq, sk = (B, Hq, N, d), (B, p.Hkv, x.M, d)

@@ -473,7 +473,7 @@ static int make_cross(const psa_params* p, const psa_cross* x, Plan* pl, CrossCa
 
 int psa_query_cross_sizes(const psa_params* p, const psa_cross* x, size_t* fwd_scratch, size_t* bwd_scratch) {
   Plan pl;
-  CrossCall c;
+  CrossCall c = {};
   const int rc = make_cross(p, x, &pl, &c, true);
   if (rc != PSA_OK) return rc;
   auto most = [](size_t u, size_t v) { return u > v ? u : v; };
@@ -490,7 +490,7 @@ int psa_query_cross_sizes(const psa_params* p, const psa_cross* x, size_t* fwd_s
 int psa_cross_attention_fwd(const psa_params* p, const psa_cross* x, const void* Q, const void* K, const void* V, const int32_t* kv_len,
                             const uint8_t* key_mask, void* O, float* lse, void* scratch, void* stream) {
   Plan pl;
-  CrossCall c;
+  CrossCall c = {};
   const int rc = make_cross(p, x, &pl, &c, false);
   if (rc != PSA_OK) return rc;
   if (!Q || !O || (c.M > 0 && (!K || !V)) || O == Q || O == K || O == V) return PSA_EINVAL;
@@ -507,7 +507,7 @@ int psa_cross_attention_bwd(const psa_params* p, const psa_cross* x, const void*
                             const uint8_t* key_mask, const void* O, const float* lse, const void* dO, void* dQ, void* dK, void* dV,
                             void* scratch, void* stream) {
   Plan pl;
-  CrossCall c;
+  CrossCall c = {};
   const int rc = make_cross(p, x, &pl, &c, true);
   if (rc != PSA_OK) return rc;
   if (!Q || !O || !lse || !dO || !dQ || !scratch || (c.M > 0 && (!K || !V || !dK || !dV))) return PSA_EINVAL;

@@ -313,6 +313,31 @@ def test_bits_repeat_on_other_streams_and_in_graphs(dtype, N, M):
         assert all(torch.equal(u, v) for u, v in zip(got, want[0])) == (turn != 1)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_two_graphs_share_a_workspace(dtype):
+    """Problems of other sizes whose calls leave partial results in the same memory, replayed by turns on one stream, with an eager call between."""
+    import torch
+    a, b = Problem(dtype, 64, 1, 2, 2, 20, 3000, seed=3), Problem(dtype, 64, 2, 2, 1, 700, 150, lengths=[150, 9], seed=60)
+    shared = [scratch(max(x.ws[i].numel() for x in (a, b))) for i in (0, 1)]
+    graphs, want = [], []
+    for x in (a, b):
+        x.check()
+        want.append([t.clone() for t in (x.O, x.lse, *x.grads)])
+        x.ws = shared
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            x.forward()
+            x.backward()
+    for turn in (0, 1, 1, 0, 1, 0):
+        x = (a, b)[turn]
+        for t in (x.O, x.lse, *x.grads):
+            t.fill_(3.0)
+        graphs[turn].replay()
+        (b, a)[turn].forward()
+        torch.cuda.synchronize()
+        assert all(torch.equal(u, v) for u, v in zip((x.O, x.lse, *x.grads), want[turn]))
+
+
 def test_gradients_against_differences():
     """float32: (f(x + h) - f(x - h)) / 2h of <O, dO> summed in 64 bits. The outputs are off by at most bO, so the slope by sum bO |dO| / h, and by h^2 / 6 times a third
     derivative, for which 50 stands (inputs of size one, 12 states)."""
