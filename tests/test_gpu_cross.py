@@ -165,6 +165,34 @@ def test_offsets_beyond_32_bits(dtype, d):
     a.check()
 
 
+def test_as_many_heads_as_a_call_takes():
+    """65535 key heads of one or two rows and few states, float32, against 64 bits on the GPU; one more is refused."""
+    import torch
+    B, H, N, M, d = 4369, 15, 2, 5, 64
+    p = params("f32", B, H, H, N, d)
+    gen = torch.Generator("cuda").manual_seed(5)
+    Q, K, V, dO = (torch.randn((B, H, n, d), generator=gen, device="cuda") for n in (N, M, M, N))
+    O, lse, grads = torch.empty_like(Q), torch.empty((B, H, N), device="cuda"), [torch.empty_like(x) for x in (Q, K, V)]
+    x = psa.make_cross(M)
+    fwd, bwd = psa.psa_query_cross_sizes(p, x)
+    psa.psa_cross_attention_fwd(p, x, Q, K, V, O, scratch(fwd), lse=lse)
+    psa.psa_cross_attention_bwd(p, x, Q, K, V, O, lse, dO, *grads, scratch(bwd))
+    q, k, v, g, o = (t.double() for t in (Q, K, V, dO, O))
+    s = (q[:, :, :, None] * k[:, :, None]).sum(-1) / 8
+    w = torch.softmax(s, -1)
+    # a score is off by its 64 products and sums, the rest by fewer than 40 roundings of its terms
+    u = 2.0 ** -24
+    delta = u * ((d + 4) * (q.abs()[:, :, :, None] * k.abs()[:, :, None]).sum(-1).max() / 8 + 8 * (1 + s.abs().max()))
+    assert torch.all((lse.double() - torch.logsumexp(s, -1)).abs() <= delta + 40 * u)
+    want, size = ((w[..., None] * t[:, :, None]).sum(3) for t in (v, v.abs()))
+    assert torch.all((o - want).abs() <= size * (2 * delta + 40 * u))
+    p_ = torch.exp(s - lse.double()[..., None])
+    dv, size = ((p_[..., None] * t[:, :, :, None]).sum(2) for t in (g, g.abs()))
+    assert torch.all((grads[2].double() - dv).abs() <= size * (2 * delta + 40 * u))
+    with pytest.raises(psa.PsaError):
+        psa.psa_query_cross_sizes(params("f32", B + 1, H, H, N, d), x)
+
+
 def test_states_beyond_the_cache():
     """A row or three against 300 MB of states, lengths that end in the last part: against 64 bits on the GPU, a head at a time."""
     import torch
